@@ -304,6 +304,117 @@ tpdq_status tpdq_gated_mlp_shard(const void* X, int64_t ldx, int32_t M, const in
  * arguments are invalid. */
 size_t tpdq_workspace_bytes(int op, int32_t M, const tpdq_w4* a, const tpdq_w4* b);
 
+/* ---- Microscaled (MX) operands --------------------------------------------
+ *
+ * The layer's other 4-bit form: floating-point codes with one power-of-two
+ * scale per 32 consecutive elements of a row (the OCP microscaling formats),
+ * which gfx950's matrix instructions multiply without dequantizing. Weights are
+ * fp4; activations are fp8 or fp4, quantized from 16 bits by tpdq_mx_quantize or
+ * by tpdq_rmsnorm in one pass with the norm before the layer. There is no
+ * act-order: rows need no permutation.
+ *
+ * Element formats. TPDQ_MX_FP4: E2M1, values 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives, two codes to a byte, the even element in the low half.
+ * TPDQ_MX_FP8: E4M3, one byte, largest value 448, no infinity, NaN 0x7F.
+ * Scales: E8M0, one byte b = 2^(b - 127), 255 = NaN (all the block's values). */
+typedef enum { TPDQ_MX_FP4 = 0, TPDQ_MX_FP8 = 1 } tpdq_mx_format;
+
+/* Storage of an R x K tensor (bytes; every pointer and leading dimension a
+ * multiple of 16).
+ * TPDQ_MX_ROWS: codes [R][ld_c], element k of a row in byte k (fp8) or k / 2
+ *   (fp4); scales [R][ld_s], elements 32 b .. 32 b + 31 in byte b. A row is padded:
+ *   ld_c >= 128 ceil(K/128) elements, ld_s >= 16 ceil(K/512); the products read the
+ *   padding, whose codes and scales must be zero (quantize and rmsnorm write it).
+ * TPDQ_MX_TILED (weights, fp4): codes [ceil(R/32)][ld_c], ld_c >= 2048
+ *   ceil(K/128); scales [ceil(R/32)][ld_s], ld_s >= 512 ceil(K/512). For 32-row tile
+ *   T, 128-element step s, operand j (0, 1) and lane l = 16 g + i (i < 16, g < 4), with
+ *   row n = 32 T + 8 (i / 4) + 4 j + i % 4:
+ *     the 16 bytes at codes + T ld_c + 2048 s + 1024 j + 16 l are row n's elements
+ *       128 s + 32 g .. + 31;
+ *     byte t of the word at scales + T ld_s + 512 c + 8 l + 4 j is the scale of row
+ *       n's elements 512 c + 128 t + 32 g .. + 31.
+ *   Codes and scales past R or K are zero. Rows cut at multiples of 32 and columns
+ *   cut at multiples of 512 are views. Made by tpdq_mx_pack. */
+typedef enum { TPDQ_MX_ROWS = 0, TPDQ_MX_TILED = 1 } tpdq_mx_layout;
+
+/* R and K are positive, K a multiple of 8 (a last block of 8, 16 or 24 elements
+ * has zero codes behind them). */
+typedef struct tpdq_mx {
+  void* codes;
+  int64_t ld_c;
+  void* scales;
+  int64_t ld_s;
+  int32_t R;
+  int32_t K;
+  int32_t format; /* tpdq_mx_format */
+  int32_t layout; /* tpdq_mx_layout */
+} tpdq_mx;
+
+/*
+ * tpdq_mx_quantize - q = X in q's format (TPDQ_MX_ROWS), X [q->R][ldx] in 16
+ * bits with q->K columns used. Per block of 32 (of a last block: what there is):
+ *   scale = 2^e, e = floor(log2(max |x|)) - 2 (fp4) or - 8 (fp8), at least -127
+ *   code  = x / scale rounded to nearest, ties to even, saturating at 6 or 448.
+ * A block of zeros has scale 2^-127. A block that holds a NaN or an infinity has
+ * scale NaN and zero codes. Alignment: X 16 B, ldx % 8 == 0.
+ */
+tpdq_status tpdq_mx_quantize(const void* X, int64_t ldx, tpdq_dtype dtype, const tpdq_mx* q, void* stream);
+
+/* tpdq_mx_dequantize - X [q->R][ldx] = the values of q (TPDQ_MX_ROWS), code times
+ * scale rounded once to 16 bits. Alignment of X as for tpdq_mx_quantize. */
+tpdq_status tpdq_mx_dequantize(const tpdq_mx* q, tpdq_dtype dtype, void* X, int64_t ldx, void* stream);
+
+/* tpdq_mx_pack - copy an fp4 tensor from TPDQ_MX_ROWS (src) to TPDQ_MX_TILED (dst,
+ * the same R and K). Offline; asynchronous on `stream`. */
+tpdq_status tpdq_mx_pack(const tpdq_mx* src, const tpdq_mx* dst, void* stream);
+
+/*
+ * tpdq_rmsnorm - the norm before the layer, with the residual's addition:
+ *   h = X + residual, rounded to dtype and written to residual_out (h = X without
+ *       a residual; both must then be NULL)
+ *   y = h / sqrt(mean(h^2) + eps) * weight, in fp32
+ * y goes to Y [M][ldy] rounded to dtype (then q is NULL), as tpdq_w4a16_gemm and
+ * the MLP shards take it, or to q (TPDQ_MX_ROWS, R = M; then Y is NULL), quantized
+ * from fp32 as by tpdq_mx_quantize. X, residual [M][ld] and weight [K] are of
+ * dtype. residual_out may be residual itself. K a multiple of 8, at most 65536. The
+ * sum of squares is taken in fp32: rows of magnitudes past 2^63 / sqrt(K) overflow it.
+ * Alignment: every pointer 16 B, every leading dimension % 8 == 0.
+ */
+tpdq_status tpdq_rmsnorm(const void* X, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                         float eps, int32_t M, int32_t K, tpdq_dtype dtype, void* residual_out, int64_t ldh,
+                         void* Y, int64_t ldy, const tpdq_mx* q, void* stream);
+
+/*
+ * tpdq_mx_gemm - Y = X W^T: X [M][K] (TPDQ_MX_ROWS, fp8 or fp4), w [N][K]
+ * (TPDQ_MX_TILED, fp4), fp32 accumulation over all of K, Y [M][ldy] rounded once to
+ * dtype (fp16 or bf16). M = X->R, N = w->R, a multiple of 8; X->K == w->K. Alignment:
+ * Y 16 B, ldy % 8 == 0. A NaN (a code's or a scale's) in row m of X gives NaN in row
+ * m of Y alone, in row n of w in column n alone. Deterministic.
+ * Workspace: tpdq_mx_workspace_bytes(0, M, w, NULL) bytes, any content. Calls that
+ * overlap in time must not share a workspace.
+ */
+tpdq_status tpdq_mx_gemm(const tpdq_mx* X, const tpdq_mx* w, tpdq_dtype dtype, void* Y, int64_t ldy,
+                         void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * tpdq_mx_mlp_shard - one rank's share of the MLP up to its AllReduce, in MX:
+ *   Y1 = X w_up^T, or silu(X w_gate^T) * (X w_up^T) when w_gate is given, in fp32,
+ *        quantized in X's format as by tpdq_mx_quantize;
+ *   Y2_partial = Y1 w_down^T, [X->R][w_down->R], dense, rounded once to dtype.
+ * w_gate and w_up are the rank's rows (outputs) of the whole projections, w_down
+ * its columns (inputs): w_down->K == w_up->R. w_gate must have w_up's R, K and
+ * leading dimensions. Other requirements as for tpdq_mx_gemm.
+ * Workspace: tpdq_mx_workspace_bytes(1, M, w_up, w_down) bytes, any content (it
+ * holds Y1).
+ */
+tpdq_status tpdq_mx_mlp_shard(const tpdq_mx* X, const tpdq_mx* w_gate, const tpdq_mx* w_up, const tpdq_mx* w_down,
+                              tpdq_dtype dtype, void* Y2_partial, void* workspace, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for op 0 (tpdq_mx_gemm: a = w) or 1 (tpdq_mx_mlp_shard: a =
+ * w_up, b = w_down) at batch M, whatever X's format. 0 when the arguments are
+ * invalid, or when the call needs none. */
+size_t tpdq_mx_workspace_bytes(int op, int32_t M, const tpdq_mx* a, const tpdq_mx* b);
+
 /* Static description of a status code. */
 const char* tpdq_status_string(tpdq_status s);
 

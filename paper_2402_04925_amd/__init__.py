@@ -12,14 +12,16 @@ import dataclasses
 from typing import Optional
 
 from . import _abi
-from ._abi import (BF16, FP16, LAYOUT_GPTQ, LAYOUT_TILED, OP_GATED_MLP, OP_GEMM, OP_MLP, OP_REORDER,
-                   PATH_ACTORDER, PATH_ACTORDER_GLOBAL, PATH_ORDERED, TpdqError)
+from ._abi import (BF16, FP16, LAYOUT_GPTQ, LAYOUT_TILED, MX_FP4, MX_FP8, MX_ROWS, MX_TILED,
+                   OP_GATED_MLP, OP_GEMM, OP_MLP, OP_REORDER, PATH_ACTORDER, PATH_ACTORDER_GLOBAL, PATH_ORDERED, TpdqError)
 
 __all__ = [
     "QuantWeight", "reorder", "pack_tiled", "w4a16_gemm", "mlp_shard", "mlp_shard_noalloc",
     "gated_mlp_shard",
     "workspace_bytes", "Workspace",
     "LAYOUT_GPTQ", "LAYOUT_TILED", "tiled_ld",
+    "MxTensor", "mx_quantize", "mx_dequantize", "mx_pack", "rmsnorm", "mx_gemm", "mx_mlp_shard",
+    "MX_FP4", "MX_FP8", "MX_ROWS", "MX_TILED",
     "TpdqError", "PATH_ACTORDER", "PATH_ORDERED", "PATH_ACTORDER_GLOBAL", "FP16", "BF16", "version",
 ]
 
@@ -399,3 +401,7 @@ def gated_mlp_shard(X, w_gate: QuantWeight, w_up: QuantWeight, w_down: QuantWeig
         _ptr(X), X.stride(0), M, _ptr(P1), ctypes.byref(cg), ctypes.byref(cu), ctypes.byref(cd), path,
         _dtype_code(X.dtype), _ptr(y1), _ptr(y2), _ptr(buf), buf.numel(), _stream_handle(X.device)))
     return y1, y2
+
+
+from .mx import (MxTensor, mx_dequantize, mx_gemm, mx_mlp_shard, mx_pack, mx_quantize,  # noqa: E402
+                 rmsnorm)

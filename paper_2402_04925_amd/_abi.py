@@ -12,11 +12,16 @@ FP16, BF16 = 0, 1
 PATH_ACTORDER, PATH_ORDERED, PATH_ACTORDER_GLOBAL = 0, 1, 2
 OP_REORDER, OP_GEMM, OP_MLP, OP_GATED_MLP = 0, 1, 2, 3
 LAYOUT_GPTQ, LAYOUT_TILED = 0, 1
+MX_FP4, MX_FP8 = 0, 1
+MX_ROWS, MX_TILED = 0, 1
+OP_MX_GEMM, OP_MX_MLP = 0, 1  # of tpdq_mx_workspace_bytes
 
 EXPORTED = (
     "tpdq_reorder", "tpdq_pack_tiled", "tpdq_w4a16_gemm", "tpdq_mlp_shard", "tpdq_mlp_shard_noalloc",
     "tpdq_gated_mlp_shard",
     "tpdq_workspace_bytes",
+    "tpdq_mx_quantize", "tpdq_mx_dequantize", "tpdq_mx_pack", "tpdq_rmsnorm", "tpdq_mx_gemm", "tpdq_mx_mlp_shard",
+    "tpdq_mx_workspace_bytes",
     "tpdq_status_string", "tpdq_last_error", "tpdq_version",
 )
 
@@ -31,6 +36,16 @@ class W4(ctypes.Structure):
         ("K", ctypes.c_int32), ("N", ctypes.c_int32),
         ("group_size", ctypes.c_int32), ("num_groups", ctypes.c_int32),
         ("layout", ctypes.c_int32), ("zero_offset", ctypes.c_int32),
+    ]
+
+
+class Mx(ctypes.Structure):
+    """struct tpdq_mx."""
+    _fields_ = [
+        ("codes", ctypes.c_void_p), ("ld_c", ctypes.c_int64),
+        ("scales", ctypes.c_void_p), ("ld_s", ctypes.c_int64),
+        ("R", ctypes.c_int32), ("K", ctypes.c_int32),
+        ("format", ctypes.c_int32), ("layout", ctypes.c_int32),
     ]
 
 
@@ -60,6 +75,21 @@ def _declare(lib):
     lib.tpdq_gated_mlp_shard.restype = ctypes.c_int
     lib.tpdq_workspace_bytes.argtypes = [ctypes.c_int, i32, pw, pw]
     lib.tpdq_workspace_bytes.restype = sz
+    pm, f32 = ctypes.POINTER(Mx), ctypes.c_float
+    lib.tpdq_mx_quantize.argtypes = [vp, i64, ctypes.c_int, pm, vp]
+    lib.tpdq_mx_quantize.restype = ctypes.c_int
+    lib.tpdq_mx_dequantize.argtypes = [pm, ctypes.c_int, vp, i64, vp]
+    lib.tpdq_mx_dequantize.restype = ctypes.c_int
+    lib.tpdq_mx_pack.argtypes = [pm, pm, vp]
+    lib.tpdq_mx_pack.restype = ctypes.c_int
+    lib.tpdq_rmsnorm.argtypes = [vp, i64, vp, i64, vp, f32, i32, i32, ctypes.c_int, vp, i64, vp, i64, pm, vp]
+    lib.tpdq_rmsnorm.restype = ctypes.c_int
+    lib.tpdq_mx_gemm.argtypes = [pm, pm, ctypes.c_int, vp, i64, vp, sz, vp]
+    lib.tpdq_mx_gemm.restype = ctypes.c_int
+    lib.tpdq_mx_mlp_shard.argtypes = [pm, pm, pm, pm, ctypes.c_int, vp, vp, sz, vp]
+    lib.tpdq_mx_mlp_shard.restype = ctypes.c_int
+    lib.tpdq_mx_workspace_bytes.argtypes = [ctypes.c_int, i32, pm, pm]
+    lib.tpdq_mx_workspace_bytes.restype = sz
     lib.tpdq_status_string.argtypes = [ctypes.c_int]
     lib.tpdq_status_string.restype = ctypes.c_char_p
     lib.tpdq_last_error.argtypes = []

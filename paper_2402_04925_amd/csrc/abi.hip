@@ -8,6 +8,7 @@
 #include <mutex>
 #include <string>
 
+#include "mx_internal.h"
 #include "tpdq_internal.h"
 
 using namespace tpdq;
@@ -26,6 +27,10 @@ namespace {
 
 thread_local std::string g_last_error;
 
+}  // namespace
+
+namespace tpdq {
+
 tpdq_status fail(tpdq_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -39,6 +44,10 @@ tpdq_status fail(tpdq_status st, const char* fmt, ...) {
 tpdq_status hip_fail(hipError_t e, const char* what) {
   return fail(TPDQ_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace tpdq
+
+namespace {
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 

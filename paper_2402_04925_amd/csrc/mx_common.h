@@ -1,0 +1,132 @@
+// Device helpers of the microscaled (MX) kernels: the scale of a block and the
+// conversion to its elements, and the scaled matrix instruction.
+#pragma once
+
+#include "kernels_common.h"
+#include "mx_internal.h"
+
+namespace tpdq {
+namespace {
+
+constexpr int kFp4 = TPDQ_MX_FP4;
+constexpr int kFp8 = TPDQ_MX_FP8;
+
+typedef int i8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t u2_t __attribute__((ext_vector_type(2)));
+typedef short s2_t __attribute__((ext_vector_type(2)));
+
+// The largest power of two of the element formats: 4 = 2^2 and 256 = 2^8
+template <int FMT>
+constexpr int kMxTop = FMT == kFp4 ? 2 : 8;
+
+// |x| as an ordered integer: NaN above infinity above every finite value, so
+// that one maximum finds the block's largest magnitude and what is not finite
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
+
+// E8M0 scale byte of a block whose largest magnitude has these bits: 2^(byte -
+// 127) with byte - 127 = floor(log2(max)) - kMxTop, at least -127 (also for a
+// block of zeros); 255, NaN, where the block holds a NaN or an infinity.
+template <int FMT>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t max_bits) {
+  const uint32_t e = max_bits >> 23;  // of a subnormal maximum 0: the clamp's side
+  if (e == 255u) return 255u;
+  return e > (uint32_t)kMxTop<FMT> ? e - (uint32_t)kMxTop<FMT> : 0u;
+}
+
+// What x is multiplied by before it is rounded to the grid: 1 / 2^(byte - 127),
+// a normal number for every byte up to 252, the largest that scale_byte gives.
+// A block of scale NaN keeps zeros as its codes.
+__device__ __forceinline__ float scale_inverse(uint32_t byte) {
+  return byte == 255u ? 0.f : as_f32((254u - byte) << 23);
+}
+
+// 8 elements of a lane -> codes, nearest even and saturating at the format's
+// largest value: 8 bytes of fp8 (r.x, r.y) or 4 of fp4 (r.x).
+template <int FMT>
+__device__ __forceinline__ u2_t mx_codes8(const float (&v)[8], uint32_t byte) {
+  const float inv = scale_inverse(byte);
+  float t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = byte == 255u ? 0.f : v[i] * inv;
+  u2_t r = {0u, 0u};
+  if constexpr (FMT == kFp4) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[0], t[1], 1.f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[2], t[3], 1.f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[4], t[5], 1.f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, t[6], t[7], 1.f, 3);
+    r.x = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = __builtin_amdgcn_fmed3f(t[i], -448.f, 448.f);  // the conversion gives NaN past it
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s2_t p = {0, 0};
+      p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, t[4 * i], t[4 * i + 1], 1.f, false);
+      p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, t[4 * i + 2], t[4 * i + 3], 1.f, true);
+      r[i] = __builtin_bit_cast(uint32_t, p);
+    }
+  }
+  return r;
+}
+
+template <int FMT>
+__device__ __forceinline__ uint32_t max_bits8(const float (&v)[8]) {
+  uint32_t m = abs_bits(v[0]);
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = max(m, abs_bits(v[i]));
+  return m;
+}
+
+template <int DT>
+__device__ __forceinline__ void unpack8(u4_t x, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = x[i];
+    v[2 * i] = bits_to_float<DT>(w & 0xFFFFu);
+    v[2 * i + 1] = bits_to_float<DT>(w >> 16);
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ u4_t pack8(const float (&v)[8]) {
+  u4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = pack2<DT>(v[2 * i], v[2 * i + 1]);
+  return r;
+}
+
+// The 8 codes and, from the block's first lane (k8 % 4 == 0), the scale of
+// elements 8 k8 .. 8 k8 + 7 of a row. The four lanes of a block are consecutive
+// and run this together; codes past the row's padding to whole steps are not
+// there to be written (their chunk's scales are).
+template <int FMT>
+__device__ __forceinline__ void store_mx8(const float (&v)[8], int k8, int code_octets, uint8_t* codes,
+                                          uint8_t* scales) {
+  uint32_t m = max_bits8<FMT>(v);
+  m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+  m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+  const uint32_t byte = scale_byte<FMT>(m);
+  const u2_t c = mx_codes8<FMT>(v, byte);
+  if (k8 < code_octets) {
+    if constexpr (FMT == kFp4) *(uint32_t*)(codes + 4 * (int64_t)k8) = c.x;
+    else *(u2_t*)(codes + 8 * (int64_t)k8) = c;
+  }
+  if ((k8 & 3) == 0) scales[k8 >> 2] = (uint8_t)byte;
+}
+
+// acc += W (16 rows, fp4) X^T (16 rows, FMT): 128 elements of K. Lane (r, g) =
+// (lane % 16, lane / 16) holds of row r: fp4 elements 32 g .. 32 g + 31 (4
+// words); fp8 elements 16 g .. 16 g + 15 (words 0 .. 3) and 64 + 16 g .. (words
+// 4 .. 7); in its scale word the byte of elements 32 g .. 32 g + 31. Result:
+// lane (m, g) holds outputs 4 g .. 4 g + 3 of X's row m.
+// WSEL: which byte of the weights' scale word.
+template <int FMT, int WSEL>
+__device__ __forceinline__ f4_t mfma_mx(u4_t w, uint32_t wscale, i8_t x, uint32_t xscale, f4_t acc) {
+  i8_t a = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, x, acc, 4, FMT == kFp4 ? 4 : 0, WSEL, (int)wscale, 0,
+                                                          (int)xscale);
+}
+
+}  // namespace
+}  // namespace tpdq

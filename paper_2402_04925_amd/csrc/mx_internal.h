@@ -1,0 +1,77 @@
+// Internal declarations of the microscaled (MX) operators: launch descriptions
+// shared by mx_abi.hip (validation, dispatch), mx_rows.hip (row-wise kernels)
+// and the product's kernels.
+#pragma once
+
+#include "tpdq_internal.h"
+
+namespace tpdq {
+
+// abi.hip: sets tpdq_last_error() and returns st
+tpdq_status fail(tpdq_status st, const char* fmt, ...);
+tpdq_status hip_fail(hipError_t e, const char* what);
+
+// Elements per scale; elements of one matrix instruction's K step; of the run of
+// steps whose scales one 32-bit word per lane holds.
+constexpr int kMxBlock = 32;
+constexpr int kMxStep = 128;
+constexpr int kMxChunk = 512;
+constexpr int kMxTile = 32;  // weight rows (outputs) of a tile: two 16-row operands
+
+inline int64_t mx_steps(int64_t K) { return (K + kMxStep - 1) / kMxStep; }
+inline int64_t mx_chunks(int64_t K) { return (K + kMxChunk - 1) / kMxChunk; }
+// bytes of one row's codes and scales (TPDQ_MX_ROWS), padding included
+inline int64_t mx_row_codes(int64_t K, int fmt) { return mx_steps(K) * (fmt == TPDQ_MX_FP4 ? 64 : 128); }
+inline int64_t mx_row_scales(int64_t K) { return mx_chunks(K) * 16; }
+// bytes of one 32-row tile's codes and scales (TPDQ_MX_TILED)
+inline int64_t mx_tile_codes(int64_t K) { return mx_steps(K) * 2048; }
+inline int64_t mx_tile_scales(int64_t K) { return mx_chunks(K) * 512; }
+
+struct MxRows {  // a TPDQ_MX_ROWS tensor
+  uint8_t* codes;
+  int64_t ld_c;
+  uint8_t* scales;
+  int64_t ld_s;
+};
+
+hipError_t launch_mx_quantize(const uint16_t* X, int64_t ldx, int R, int K, int dt, int fmt, const MxRows& q,
+                              hipStream_t s);
+hipError_t launch_mx_dequantize(const MxRows& q, int R, int K, int dt, int fmt, uint16_t* X, int64_t ldx,
+                                hipStream_t s);
+hipError_t launch_mx_pack(const MxRows& q, int R, int K, uint8_t* codes, int64_t ld_c, uint8_t* scales,
+                          int64_t ld_s, hipStream_t s);
+
+// Columns of a row that k_rmsnorm holds in a workgroup's registers
+constexpr int kNormMaxK = 65536;
+struct NormArgs {
+  const uint16_t* X;
+  int64_t ldx;
+  const uint16_t* res;  // or NULL
+  int64_t ldr;
+  const uint16_t* w;
+  uint16_t* h;  // X + res in 16 bits, or NULL
+  int64_t ldh;
+  uint16_t* Y;  // 16-bit output, or NULL with q
+  int64_t ldy;
+  MxRows q;
+  int M, K;
+  float eps;
+};
+hipError_t launch_rmsnorm(const NormArgs& a, int dt, int fmt, hipStream_t s);  // fmt < 0: 16 bits
+
+// One product Y = X W^T (device pointers).
+struct MxArgs {
+  MxRows x;            // [M][K], fp8 or fp4
+  const uint8_t* wc;   // TPDQ_MX_TILED, fp4: [ceil(N/32)][ldwc]
+  const uint8_t* ws;
+  const uint8_t* wc_up;  // gated: the up projection, with the same leading dimensions
+  const uint8_t* ws_up;
+  int64_t ldwc, ldws;
+  int M, N, K;
+  uint16_t* Y;  // 16-bit output [M][ldy], or NULL with q
+  int64_t ldy;
+  MxRows q;     // output in X's format
+};
+hipError_t launch_mx_gemm(const MxArgs& a, int dt, int fmt, hipStream_t s);
+
+}  // namespace tpdq
