@@ -128,5 +128,26 @@ __device__ __forceinline__ f4_t mfma_mx(u4_t w, uint32_t wscale, i8_t x, uint32_
                                                           (int)xscale);
 }
 
+// 8 outputs of a lane in 16 bits, or quantized into X's format (the block's four
+// lanes are 16 apart). n: the first output; rows past M write nothing.
+template <int DT, int FMT, bool QUANT>
+__device__ __forceinline__ void store_out8(const MxArgs& a, const float (&v)[8], int m, int64_t n) {
+  if constexpr (QUANT) {
+    uint32_t mb = max_bits8<FMT>(v);
+    mb = max(mb, (uint32_t)__shfl_xor((int)mb, 16));
+    mb = max(mb, (uint32_t)__shfl_xor((int)mb, 32));
+    const uint32_t byte = scale_byte<FMT>(mb);
+    const u2_t c = mx_codes8<FMT>(v, byte);
+    if (m >= a.M) return;
+    if (n < (int64_t)(a.N + kMxStep - 1) / kMxStep * kMxStep) {
+      if constexpr (FMT == kFp4) *(uint32_t*)(a.q.codes + (int64_t)m * a.q.ld_c + n / 2) = c.x;
+      else *(u2_t*)(a.q.codes + (int64_t)m * a.q.ld_c + n) = c;
+    }
+    if ((n & 31) == 0) a.q.scales[(int64_t)m * a.q.ld_s + (n >> 5)] = (uint8_t)byte;
+  } else {
+    if (m < a.M && n < a.N) *(u4_t*)(a.Y + (int64_t)m * a.ldy + n) = pack8<DT>(v);
+  }
+}
+
 }  // namespace
 }  // namespace tpdq

@@ -17,27 +17,6 @@
 namespace tpdq {
 namespace {
 
-// 8 outputs of a lane in 16 bits, or quantized into X's format (the block's four
-// lanes are 16 apart). n: the first output; rows past M write nothing.
-template <int DT, int FMT, bool QUANT>
-__device__ __forceinline__ void store_out8(const MxArgs& a, const float (&v)[8], int m, int64_t n) {
-  if constexpr (QUANT) {
-    uint32_t mb = max_bits8<FMT>(v);
-    mb = max(mb, (uint32_t)__shfl_xor((int)mb, 16));
-    mb = max(mb, (uint32_t)__shfl_xor((int)mb, 32));
-    const uint32_t byte = scale_byte<FMT>(mb);
-    const u2_t c = mx_codes8<FMT>(v, byte);
-    if (m >= a.M) return;
-    if (n < (int64_t)(a.N + kMxStep - 1) / kMxStep * kMxStep) {
-      if constexpr (FMT == kFp4) *(uint32_t*)(a.q.codes + (int64_t)m * a.q.ld_c + n / 2) = c.x;
-      else *(u2_t*)(a.q.codes + (int64_t)m * a.q.ld_c + n) = c;
-    }
-    if ((n & 31) == 0) a.q.scales[(int64_t)m * a.q.ld_s + (n >> 5)] = (uint8_t)byte;
-  } else {
-    if (m < a.M && n < a.N) *(u4_t*)(a.Y + (int64_t)m * a.ldy + n) = pack8<DT>(v);
-  }
-}
-
 // Few rows of X: the weight stream bounds it. A workgroup owns NP tiles of 32
 // outputs (GATED: of the gate and the up projection) over the whole of K and MT
 // tiles of 16 rows; its waves take chunks of 512 elements of K in turn, the
@@ -187,7 +166,8 @@ hipError_t rows_pick(const MxArgs& a, hipStream_t s) {
 }
 
 template <int DT, int FMT>
-hipError_t mx_gemm(const MxArgs& a, hipStream_t s) {
+hipError_t mx_gemm(const MxArgs& a, int dt, int fmt, hipStream_t s) {
+  if (a.M > 64) return launch_mx_tiles(a, dt, fmt, s);
   const bool quant = a.Y == nullptr;
   if (a.wc_up) return quant ? rows_pick<DT, FMT, true, true>(a, s) : rows_pick<DT, FMT, true, false>(a, s);
   return quant ? rows_pick<DT, FMT, false, true>(a, s) : rows_pick<DT, FMT, false, false>(a, s);
@@ -196,8 +176,8 @@ hipError_t mx_gemm(const MxArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_mx_gemm(const MxArgs& a, int dt, int fmt, hipStream_t s) {
-  if (dt == TPDQ_BF16) return fmt == TPDQ_MX_FP4 ? mx_gemm<kBF16, kFp4>(a, s) : mx_gemm<kBF16, kFp8>(a, s);
-  return fmt == TPDQ_MX_FP4 ? mx_gemm<kF16, kFp4>(a, s) : mx_gemm<kF16, kFp8>(a, s);
+  if (dt == TPDQ_BF16) return fmt == TPDQ_MX_FP4 ? mx_gemm<kBF16, kFp4>(a, dt, fmt, s) : mx_gemm<kBF16, kFp8>(a, dt, fmt, s);
+  return fmt == TPDQ_MX_FP4 ? mx_gemm<kF16, kFp4>(a, dt, fmt, s) : mx_gemm<kF16, kFp8>(a, dt, fmt, s);
 }
 
 }  // namespace tpdq

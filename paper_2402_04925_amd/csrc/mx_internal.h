@@ -73,5 +73,6 @@ struct MxArgs {
   MxRows q;     // output in X's format
 };
 hipError_t launch_mx_gemm(const MxArgs& a, int dt, int fmt, hipStream_t s);
+hipError_t launch_mx_tiles(const MxArgs& a, int dt, int fmt, hipStream_t s);  // many rows (mx_tiles.hip)
 
 }  // namespace tpdq
