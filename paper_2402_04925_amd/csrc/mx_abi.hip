@@ -92,6 +92,14 @@ MxArgs product(const MxRows& x, int M, const tpdq_mx* w, const tpdq_mx* up) {
 size_t y1_codes_bytes(int64_t M, int64_t N) { return align_up((size_t)(M * mx_row_codes(N, TPDQ_MX_FP8))); }
 size_t y1_bytes(int64_t M, int64_t N) { return y1_codes_bytes(M, N) + align_up((size_t)(M * mx_row_scales(N))); }
 
+// split-K parts of one product, for the format of X that takes more
+size_t part_bytes(int M, int N, int K, bool gated) {
+  size_t most = 0;
+  for (int fmt : {(int)TPDQ_MX_FP4, (int)TPDQ_MX_FP8})
+    most = std::max(most, mx_part_bytes(plan_mx(M, N, K, fmt, gated), M, N, gated));
+  return most;
+}
+
 bool valid_size(const tpdq_mx* w) { return w && w->R > 0 && w->K > 0 && w->K % 8 == 0 && w->R % 8 == 0; }
 
 }  // namespace
@@ -100,9 +108,11 @@ extern "C" {
 
 size_t tpdq_mx_workspace_bytes(int op, int32_t M, const tpdq_mx* a, const tpdq_mx* b) {
   if (M < 1 || !valid_size(a)) return 0;
-  if (op == 0) return 0;
+  if (op == 0) return part_bytes(M, a->R, a->K, false);
   if (op != 1 || !valid_size(b) || b->K != a->R) return 0;
-  return y1_bytes(M, a->R);
+  // Y1, then the parts of the product at hand (the first may be gated or not)
+  return y1_bytes(M, a->R) + std::max({part_bytes(M, a->R, a->K, true), part_bytes(M, a->R, a->K, false),
+                                       part_bytes(M, b->R, b->K, false)});
 }
 
 tpdq_status tpdq_mx_quantize(const void* X, int64_t ldx, tpdq_dtype dtype, const tpdq_mx* q, void* stream) {
@@ -193,10 +203,14 @@ tpdq_status tpdq_mx_gemm(const tpdq_mx* X, const tpdq_mx* w, tpdq_dtype dtype, v
   if (st == TPDQ_OK) st = check_product(X, w, "w");
   if (st == TPDQ_OK) st = check_rows16(Y, ldy, w->R, "Y");
   if (st != TPDQ_OK) return st;
+  const size_t need = tpdq_mx_workspace_bytes(0, X->R, w, nullptr);
+  if (need && (!workspace || ws_bytes < need))
+    return fail(TPDQ_ERR_WORKSPACE, "product needs %zu workspace bytes, got %zu", need, ws_bytes);
+  if (need && !aligned(workspace, 16)) return fail(TPDQ_ERR_ALIGN, "workspace needs 16-byte alignment");
   MxArgs a = product(rows_of(X), X->R, w, nullptr);
   a.Y = (uint16_t*)Y;
   a.ldy = ldy;
-  const hipError_t e = launch_mx_gemm(a, dtype, X->format, (hipStream_t)stream);
+  const hipError_t e = launch_mx_gemm(a, dtype, X->format, (float*)workspace, (hipStream_t)stream);
   return e == hipSuccess ? TPDQ_OK : hip_fail(e, "product launch");
 }
 
@@ -225,12 +239,13 @@ tpdq_status tpdq_mx_mlp_shard(const tpdq_mx* X, const tpdq_mx* w_gate, const tpd
   // gated: the gate is the first weight, up the second
   MxArgs a = w_gate ? product(rows_of(X), M, w_gate, w_up) : product(rows_of(X), M, w_up, nullptr);
   a.q = y1;
-  hipError_t e = launch_mx_gemm(a, dtype, X->format, s);
+  float* part = (float*)((char*)workspace + y1_bytes(M, N1));
+  hipError_t e = launch_mx_gemm(a, dtype, X->format, part, s);
   if (e != hipSuccess) return hip_fail(e, "first product launch");
   MxArgs d = product(y1, M, w_down, nullptr);
   d.Y = (uint16_t*)Y2_partial;
   d.ldy = w_down->R;
-  e = launch_mx_gemm(d, dtype, X->format, s);
+  e = launch_mx_gemm(d, dtype, X->format, part, s);
   return e == hipSuccess ? TPDQ_OK : hip_fail(e, "second product launch");
 }
 

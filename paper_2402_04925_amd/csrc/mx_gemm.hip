@@ -165,19 +165,30 @@ hipError_t rows_pick(const MxArgs& a, hipStream_t s) {
   return rows_launch<DT, FMT, 4, 1, GATED, QUANT, 8>(a, s);
 }
 
-template <int DT, int FMT>
-hipError_t mx_gemm(const MxArgs& a, int dt, int fmt, hipStream_t s) {
-  if (a.M > 64) return launch_mx_tiles(a, dt, fmt, s);
-  const bool quant = a.Y == nullptr;
-  if (a.wc_up) return quant ? rows_pick<DT, FMT, true, true>(a, s) : rows_pick<DT, FMT, true, false>(a, s);
-  return quant ? rows_pick<DT, FMT, false, true>(a, s) : rows_pick<DT, FMT, false, false>(a, s);
+template <int FMT>
+hipError_t rows_of(const MxArgs& a, int dt, hipStream_t s) {
+  if (a.wc_up) return rows_pick<kF16, FMT, true, true>(a, s);
+  if (!a.Y) return rows_pick<kF16, FMT, false, true>(a, s);
+  return dt == TPDQ_BF16 ? rows_pick<kBF16, FMT, false, false>(a, s) : rows_pick<kF16, FMT, false, false>(a, s);
 }
 
 }  // namespace
 
-hipError_t launch_mx_gemm(const MxArgs& a, int dt, int fmt, hipStream_t s) {
-  if (dt == TPDQ_BF16) return fmt == TPDQ_MX_FP4 ? mx_gemm<kBF16, kFp4>(a, dt, fmt, s) : mx_gemm<kBF16, kFp8>(a, dt, fmt, s);
-  return fmt == TPDQ_MX_FP4 ? mx_gemm<kF16, kFp4>(a, dt, fmt, s) : mx_gemm<kF16, kFp8>(a, dt, fmt, s);
+MxPlan plan_mx(int M, int N, int K, int fmt, bool gated) {
+  if (M <= 64) return MxPlan{0, 1};
+  return MxPlan{M <= 128 ? 3 : 2, 1};
+}
+
+size_t mx_part_bytes(const MxPlan& p, int M, int N, bool gated) {
+  return p.ks > 1 ? align_up((size_t)p.ks * M * N * (gated ? 8 : 4)) : 0;
+}
+
+hipError_t launch_mx_gemm(MxArgs a, int dt, int fmt, float* part, hipStream_t s) {
+  const MxPlan p = plan_mx(a.M, a.N, a.K, fmt, a.wc_up != nullptr);
+  a.ks = p.ks;
+  a.part = part;
+  if (p.bm) return launch_mx_tiles(a, p.bm, dt, fmt, s);
+  return fmt == TPDQ_MX_FP4 ? rows_of<kFp4>(a, dt, s) : rows_of<kFp8>(a, dt, s);
 }
 
 }  // namespace tpdq

@@ -71,8 +71,19 @@ struct MxArgs {
   uint16_t* Y;  // 16-bit output [M][ldy], or NULL with q
   int64_t ldy;
   MxRows q;     // output in X's format
+  float* part;  // ks > 1: [ks][(gate, up)][M][N]
+  int ks;       // K splits (tiles kernel)
 };
-hipError_t launch_mx_gemm(const MxArgs& a, int dt, int fmt, hipStream_t s);
-hipError_t launch_mx_tiles(const MxArgs& a, int dt, int fmt, hipStream_t s);  // many rows (mx_tiles.hip)
+// How a product runs: bm = 0 the few-row kernel, else tiles of bm (64, 128 or 256)
+// rows with K split over ks workgroups (fp32 parts, added in the splits' order by a
+// second kernel).
+struct MxPlan {
+  int bm, ks;
+};
+MxPlan plan_mx(int M, int N, int K, int fmt, bool gated);
+size_t mx_part_bytes(const MxPlan& p, int M, int N, bool gated);
+// part: mx_part_bytes of the plan
+hipError_t launch_mx_gemm(MxArgs a, int dt, int fmt, float* part, hipStream_t s);
+hipError_t launch_mx_tiles(const MxArgs& a, int bm, int dt, int fmt, hipStream_t s);  // mx_tiles.hip
 
 }  // namespace tpdq

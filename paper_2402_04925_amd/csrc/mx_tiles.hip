@@ -25,38 +25,46 @@ __device__ __forceinline__ int xcd_run(int b, int nb) {
   return x * q + min(x, rem) + (b >> 3);
 }
 
-template <int BYTES>
+// 16 bytes per lane from global memory straight to LDS (dst + 16 lane)
 __device__ __forceinline__ void dma_lds(__amdgpu_buffer_rsrc_t r, void* dst, uint32_t off, uint32_t soff) {
-  if constexpr (BYTES == 16)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 16, off, soff, 0, 0);
-  else
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 4, off, soff, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 16, off, soff, 0, 0);
 }
 
-template <int DT, int FMT, int RT, bool GATED, bool QUANT>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_mx_tiles(MxArgs a) {
-  constexpr int S = FMT == kFp4 ? 4 : 2;       // steps per block
-  constexpr int XW = FMT == kFp4 ? 1 : 2;      // records of a row tile per step
-  constexpr int BM = 32 * RT;
-  constexpr int XREC = RT;                     // code records (1 KB) per wave and block
-  constexpr int SREC = S * BM / 64;            // scale records (256 B) per block
-  constexpr int SPW = (SREC + 7) / 8;          // ... per wave (some twice)
-  constexpr int STAGE = BM * 256 + SREC * 256;
-  constexpr int ITEMS = XREC + SPW;            // loads to LDS per wave and block
+template <int DT, int FMT, int RT, int WM, int NP, int NW, int S, bool GATED, bool QUANT>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_mx_tiles(MxArgs a) {
+  static_assert(!GATED || NP == 2, "a tile of the gate and one of the up projection");
+  constexpr int WN = NW / WM;
+  constexpr int NT = 2 * NP;  // operands per wave
+  constexpr int XW = FMT == kFp4 ? 1 : 2;      // 64-byte halves of a row's line per step
+  constexpr int REC = S * XW;                  // code records (1 KB) of a row tile per block
+  constexpr int BM = 16 * RT * WM;
+  static_assert(BM % 64 == 0 && (RT * WM * REC) % NW == 0 && (S == 2 || S == 4), "whole records, evenly over the waves");
+  constexpr int XREC = RT * WM * REC / NW;     // ... per wave and block
+  constexpr int SREC = BM / 64;                // scale records (1 KB), one for each of the first waves
+  static_assert(SREC <= NW, "");
+  constexpr int XBYTES = BM * REC * 64;
+  constexpr int STAGE = XBYTES + SREC * 1024;
+  constexpr int ITEMS = XREC + 1;              // loads to LDS per wave and block
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave >> 2, wn = wave & 3;
+  const int wm = wave / WN, wn = wave % WN;
   const int r16 = lane & 15, g = lane >> 4;
   const int nbm = (a.M + BM - 1) / BM;
-  const int tl = xcd_run(blockIdx.x, gridDim.x);
+  const int ks = a.ks;
+  const int ntl = (int)(gridDim.x / ks);  // output tiles; neighbours take one split's X
+  const int lt = xcd_run(blockIdx.x, gridDim.x);
+  const int kidx = lt / ntl;
+  const int tl = lt - kidx * ntl;
   const int bn = tl / nbm;
   const int row0 = (tl - bn * nbm) * BM;
-  const int T0 = GATED ? 4 * bn + wn : 8 * bn + 2 * wn;  // the wave's first 32-output tile
+  const int T0 = GATED ? WN * bn + wn : NP * (WN * bn + wn);  // the wave's first 32-output tile
   const int steps = (a.K + kMxStep - 1) / kMxStep;
   const int chunks = (a.K + kMxChunk - 1) / kMxChunk;
   const int tiles = (a.N + kMxTile - 1) / kMxTile;
-  const int nblk = (steps + S - 1) / S;
+  const int nblk_all = (steps + S - 1) / S;
+  const int kb0 = (int)((int64_t)nblk_all * kidx / ks);  // this workgroup's blocks
+  const int nblk = (int)((int64_t)nblk_all * (kidx + 1) / ks);
 
   // Rows past M and tiles past the last one load zeros from the resource bounds
   // (an offset that stays out of range whatever block is added to it); steps past
@@ -65,22 +73,20 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const uint32_t xsbytes = (uint32_t)(a.M - 1) * (uint32_t)a.x.ld_s + (uint32_t)chunks * 16u;
   const uint32_t wbytes = (uint32_t)(tiles - 1) * (uint32_t)a.ldwc + (uint32_t)steps * 2048u;
   const uint32_t wsbytes = (uint32_t)(tiles - 1) * (uint32_t)a.ldws + (uint32_t)chunks * 512u;
-  uint32_t offx[XREC], offxs[SPW], offw[2], offws[2];
+  uint32_t offx[XREC], offw[NP], offws[NP];
 #pragma unroll
   for (int k = 0; k < XREC; ++k) {
-    // record = (row tile, step, half): lane (r, g) has 16 bytes of row r
-    const int rec = XREC * wave + k, rt = rec >> 2, sh = rec & 3;
-    const int m = row0 + 16 * rt + r16;
-    offx[k] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 64u * sh + 16u * g : kOutOfRange;
+    // record = (row tile, 128-byte line, half of the rows): 8 rows of one line
+    const int rec = XREC * wave + k, rt = rec / REC, line = rec % REC / 2, hr = rec & 1;
+    const int m = row0 + 16 * rt + 8 * hr + (lane >> 3);
+    const uint32_t chunk = (uint32_t)((lane & 7) ^ (4 * hr + (lane >> 4)));
+    offx[k] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 128u * line + 16u * chunk : kOutOfRange;
   }
+  // a row's scales of the block's chunk, 16 bytes to a lane
+  const int ms = row0 + 64 * wave + lane;
+  const uint32_t offxs = wave < SREC && ms < a.M ? (uint32_t)ms * (uint32_t)a.x.ld_s : kOutOfRange;
 #pragma unroll
-  for (int k = 0; k < SPW; ++k) {
-    const int rec = (wave + 8 * k) % SREC, s = rec / (BM / 64), mb = rec % (BM / 64);
-    const int m = row0 + 64 * mb + lane;
-    offxs[k] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_s + 4u * s : kOutOfRange;
-  }
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
+  for (int p = 0; p < NP; ++p) {
     const int T = GATED ? T0 : T0 + p;
     offw[p] = T < tiles ? (uint32_t)T * (uint32_t)a.ldwc + 16u * lane : kOutOfRange;
     offws[p] = T < tiles ? (uint32_t)T * (uint32_t)a.ldws + 8u * lane : kOutOfRange;
@@ -89,15 +95,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   auto dma_item = [&](int b, int st, int k) {
     unsigned char* sb = smem + st * STAGE;
     if (k < XREC) {
-      const int sh = (XREC * wave + k) & 3;
-      const bool in = b < nblk && S * b + sh / XW < steps;
+      const int line = (XREC * wave + k) % REC / 2;
+      const bool in = b < nblk && S * b + 2 * line / XW < steps;
       const __amdgpu_buffer_rsrc_t r = buffer_rsrc(a.x.codes, in ? xbytes : 0u);
-      dma_lds<16>(r, sb + (XREC * wave + k) * 1024, offx[k], in ? 256u * (uint32_t)b : 0u);
-    } else {
-      const int rec = (wave + 8 * (k - XREC)) % SREC;
+      dma_lds(r, sb + (XREC * wave + k) * 1024, offx[k], in ? 64u * REC * (uint32_t)b : 0u);
+    } else if (wave < SREC) {
       const bool in = b < nblk;
       const __amdgpu_buffer_rsrc_t r = buffer_rsrc(a.x.scales, in ? xsbytes : 0u);
-      dma_lds<4>(r, sb + BM * 256 + rec * 256, offxs[k - XREC], in ? (uint32_t)(4 * S) * (uint32_t)b : 0u);
+      dma_lds(r, sb + XBYTES + wave * 1024, offxs, in ? (uint32_t)(S * b / 4) * 16u : 0u);
     }
   };
   auto load_w = [&](int b, int s, int i) {
@@ -115,37 +120,42 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
         r, offws[p], in ? (uint32_t)(S * b / 4) * 512u : 0u, 0));
   };
 
-  f4_t acc[RT][4];
+  // A 16-row tile's line in LDS: rows 128 bytes apart, the 16-byte chunk c of row r
+  // at place c ^ (r / 2), so that the 16 rows of one chunk lie in all 64 banks. Lane
+  // (r, g) reads chunk g (first half of the line) or 4 + g.
+  const int xpos0 = r16 * 128 + ((g ^ (r16 >> 1)) << 4), xpos1 = xpos0 ^ 64;
+
+  f4_t acc[RT][NT];
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[r][i] = f4_t{0.f, 0.f, 0.f, 0.f};
-  u4_t w[S][4];
-  u2_t ws[2], wsn[2];
+    for (int i = 0; i < NT; ++i) acc[r][i] = f4_t{0.f, 0.f, 0.f, 0.f};
+  u4_t w[S][NT];
+  u2_t ws[NP], wsn[NP];
 #pragma unroll
-  for (int k = 0; k < ITEMS; ++k) dma_item(0, 0, k);
+  for (int k = 0; k < ITEMS; ++k) dma_item(kb0, 0, k);
 #pragma unroll
-  for (int p = 0; p < 2; ++p) wsn[p] = load_ws(0, p);
+  for (int p = 0; p < NP; ++p) wsn[p] = load_ws(kb0, p);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[s][i] = load_w(0, s, i);
+    for (int i = 0; i < NT; ++i) {
+      w[s][i] = load_w(kb0, s, i);
       __builtin_amdgcn_sched_barrier(0);
     }
 
   int st = 0;
 #pragma unroll 1
-  for (int b = 0; b < nblk; ++b) {
+  for (int b = kb0; b < nblk; ++b) {
     // this wave's LDS loads of block b (and its scale words) have landed, the
     // weight loads issued after them may be in flight; the barrier publishes
     // every wave's and frees the other stage
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(4 * S) : "memory");
-    const unsigned char* xb = smem + st * STAGE + (wm * RT) * 4096;
-    const unsigned char* sb = smem + st * STAGE + BM * 256 + (wm * RT * 16 + r16) * 4 + g;
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(NT * S) : "memory");
+    const unsigned char* xb = smem + st * STAGE + wm * RT * REC * 1024;
+    const unsigned char* sb = smem + st * STAGE + XBYTES + (wm * RT * 16 + r16) * 16 + g + (S == 2 ? 8 * (b & 1) : 0);
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    for (int p = 0; p < NP; ++p) {
       ws[p] = wsn[p];
       if (S == 2 && (b & 1)) ws[p] = ws[p] >> 16;
     }
@@ -153,32 +163,33 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       constexpr int s = decltype(sel)::value;
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const u4_t lo = *(const u4_t*)(xb + (r * 4 + s * XW) * 1024 + lane * 16);
+        const unsigned char* xl = xb + (r * (REC / 2) + s * XW / 2) * 2048;
+        const u4_t lo = *(const u4_t*)(xl + (XW == 1 && s % 2 ? xpos1 : xpos0));
         u4_t hi = {0u, 0u, 0u, 0u};
-        if constexpr (XW == 2) hi = *(const u4_t*)(xb + (r * 4 + s * XW + 1) * 1024 + lane * 16);
+        if constexpr (XW == 2) hi = *(const u4_t*)(xl + xpos1);
         const i8_t x = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-        const uint32_t xs = sb[(s * BM + r * 16) * 4];
+        const uint32_t xs = sb[r * 256 + s * 4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[r][i] = mfma_mx<FMT, s>(w[s][i], ws[i >> 1][i & 1], x, xs, acc[r][i]);
+        for (int i = 0; i < NT; ++i) acc[r][i] = mfma_mx<FMT, s>(w[s][i], ws[i >> 1][i & 1], x, xs, acc[r][i]);
         if constexpr (s == 0) {  // the next block's loads to LDS, spread over the first step
 #pragma unroll
           for (int k = r * ITEMS / RT; k < (r + 1) * ITEMS / RT; ++k) dma_item(b + 1, st ^ 1, k);
           if (r == RT - 1) {
-            wsn[0] = load_ws(b + 1, 0);
-            wsn[1] = load_ws(b + 1, 1);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) wsn[p] = load_ws(b + 1, p);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < NT; ++i) {
         w[s][i] = load_w(b + 1, s, i);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
     step(std::integral_constant<int, 0>{});
     step(std::integral_constant<int, 1>{});
-    if constexpr (S == 4) {
+    if constexpr (S >= 4) {
       step(std::integral_constant<int, 2>{});
       step(std::integral_constant<int, 3>{});
     }
@@ -190,8 +201,20 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int m = row0 + (wm * RT + r) * 16 + r16;
+    if (ks > 1) {  // this split's part, [split][(gate, up)][M][N]
 #pragma unroll
-    for (int p = 0; p < (GATED ? 1 : 2); ++p) {
+      for (int p = 0; p < NP; ++p) {
+        const int64_t n = (int64_t)(GATED ? T0 : T0 + p) * kMxTile + 8 * g;
+        float* part = a.part + ((int64_t)(GATED ? 2 * kidx + p : kidx) * a.M + m) * a.N + n;
+        if (m < a.M && n < a.N) {
+          *(f4_t*)part = acc[r][2 * p];
+          *(f4_t*)(part + 4) = acc[r][2 * p + 1];
+        }
+      }
+      continue;
+    }
+#pragma unroll
+    for (int p = 0; p < (GATED ? 1 : NP); ++p) {
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -203,40 +226,95 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 }
 
-template <int DT, int FMT, int RT, bool GATED, bool QUANT>
+// Adds the splits' parts in their order and finishes the outputs: 8 of a row per
+// thread, a block of 32 in four lanes. QUANT: rows padded to whole chunks.
+template <int DT, int FMT, bool GATED, bool QUANT>
+__global__ __launch_bounds__(256) void k_mx_reduce(MxArgs a, int64_t octets, int per_row) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= octets) return;  // QUANT: whole waves
+  const int64_t m = i / per_row;
+  const int k8 = (int)(i - m * per_row);
+  float v[GATED ? 2 : 1][8];
+#pragma unroll
+  for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+    f4_t lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+    if (8 * k8 < a.N) {
+      const float* p = a.part + ((int64_t)h * a.M + m) * a.N + 8 * k8;
+      const int64_t split = (int64_t)(GATED ? 2 : 1) * a.M * a.N;
+      for (int k = 0; k < a.ks; ++k) {
+        lo += *(const f4_t*)(p + k * split);
+        hi += *(const f4_t*)(p + k * split + 4);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[h][e] = lo[e];
+      v[h][4 + e] = hi[e];
+    }
+  }
+  if constexpr (GATED) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[0][e] = silu_mul(v[0][e], v[1][e]);
+  }
+  if constexpr (QUANT)
+    store_mx8<FMT>(v[0], k8, 16 * ((a.N + kMxStep - 1) / kMxStep), a.q.codes + m * a.q.ld_c, a.q.scales + m * a.q.ld_s);
+  else
+    *(u4_t*)(a.Y + m * a.ldy + 8 * k8) = pack8<DT>(v[0]);
+}
+
+template <int DT, int FMT, int RT, int WM, int NP, int NW, int S, bool GATED, bool QUANT>
 hipError_t tiles_launch(const MxArgs& a, hipStream_t s) {
-  constexpr int S = FMT == kFp4 ? 4 : 2, BM = 32 * RT;
-  constexpr int lds = 2 * (BM * 256 + S * BM * 4);
-  auto* k = k_mx_tiles<DT, FMT, RT, GATED, QUANT>;
+  constexpr int BM = 16 * RT * WM;
+  constexpr int lds = 2 * BM * (S * (FMT == kFp4 ? 64 : 128) + 16);
+  auto* k = k_mx_tiles<DT, FMT, RT, WM, NP, NW, S, GATED, QUANT>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  const int tiles = (int)(QUANT ? mx_chunks(a.N) * (kMxChunk / kMxTile) : (a.N + kMxTile - 1) / kMxTile);
-  const int per = GATED ? 4 : 8;
-  const int64_t grid = (int64_t)((a.M + BM - 1) / BM) * ((tiles + per - 1) / per);
-  k<<<dim3((unsigned)grid), dim3(512), lds, s>>>(a);
+  const int tiles = (int)(QUANT && a.ks == 1 ? mx_chunks(a.N) * (kMxChunk / kMxTile) : (a.N + kMxTile - 1) / kMxTile);
+  const int per = (GATED ? 1 : NP) * NW / WM;
+  const int64_t grid = (int64_t)((a.M + BM - 1) / BM) * ((tiles + per - 1) / per) * a.ks;
+  k<<<dim3((unsigned)grid), dim3(NW * 64), lds, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.ks == 1) return e;
+  const int per_row = QUANT ? (int)(mx_chunks(a.N) * 64) : a.N / 8;
+  const int64_t n = (int64_t)a.M * per_row;
+  k_mx_reduce<DT, FMT, GATED, QUANT><<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(a, n, per_row);
   return hipGetLastError();
 }
 
 template <int DT, int FMT, bool GATED, bool QUANT>
-hipError_t tiles_pick(const MxArgs& a, hipStream_t s) {
-  if (a.M > 128) return tiles_launch<DT, FMT, 8, GATED, QUANT>(a, s);
-  return tiles_launch<DT, FMT, 4, GATED, QUANT>(a, s);
+hipError_t tiles_pick(const MxArgs& a, int bm, hipStream_t s) {
+  constexpr int S2 = FMT == kFp4 ? 4 : 2;
+  switch (bm) {
+    case 1: return tiles_launch<DT, FMT, 8, 2, 2, 8, S2, GATED, QUANT>(a, s);
+    case 2: return tiles_launch<DT, FMT, 8, 1, 2, 8, S2, GATED, QUANT>(a, s);
+    case 3: return tiles_launch<DT, FMT, 4, 1, 2, 8, 4, GATED, QUANT>(a, s);
+    case 4: return tiles_launch<DT, FMT, 4, 1, 2, 4, 4, GATED, QUANT>(a, s);
+    case 5: return tiles_launch<DT, FMT, 4, 2, 2, 8, 4, GATED, QUANT>(a, s);
+  }
+  if constexpr (!GATED) {
+    switch (bm) {
+      case 7: return tiles_launch<DT, FMT, 4, 1, 1, 4, 4, GATED, QUANT>(a, s);
+      case 6: return tiles_launch<DT, FMT, 8, 1, 1, 8, 4, GATED, QUANT>(a, s);
+    }
+  }
+  return hipErrorInvalidValue;
 }
 
-template <int DT, int FMT>
-hipError_t tiles_of(const MxArgs& a, hipStream_t s) {
-  const bool quant = a.Y == nullptr;
-  if (a.wc_up) return quant ? tiles_pick<DT, FMT, true, true>(a, s) : tiles_pick<DT, FMT, true, false>(a, s);
-  return quant ? tiles_pick<DT, FMT, false, true>(a, s) : tiles_pick<DT, FMT, false, false>(a, s);
+// Outputs in 16 bits, or quantized (the gated product always is: the MLP's first
+// half), which no element type enters.
+template <int FMT>
+hipError_t tiles_of(const MxArgs& a, int bm, int dt, hipStream_t s) {
+  if (a.wc_up) return tiles_pick<kF16, FMT, true, true>(a, bm, s);
+  if (!a.Y) return tiles_pick<kF16, FMT, false, true>(a, bm, s);
+  return dt == TPDQ_BF16 ? tiles_pick<kBF16, FMT, false, false>(a, bm, s) : tiles_pick<kF16, FMT, false, false>(a, bm, s);
 }
 
 }  // namespace
 
-hipError_t launch_mx_tiles(const MxArgs& a, int dt, int fmt, hipStream_t s) {
-  if (dt == TPDQ_BF16) return fmt == TPDQ_MX_FP4 ? tiles_of<kBF16, kFp4>(a, s) : tiles_of<kBF16, kFp8>(a, s);
-  return fmt == TPDQ_MX_FP4 ? tiles_of<kF16, kFp4>(a, s) : tiles_of<kF16, kFp8>(a, s);
+hipError_t launch_mx_tiles(const MxArgs& a, int bm, int dt, int fmt, hipStream_t s) {
+  return fmt == TPDQ_MX_FP4 ? tiles_of<kFp4>(a, bm, dt, s) : tiles_of<kFp8>(a, bm, dt, s);
 }
 
 }  // namespace tpdq
