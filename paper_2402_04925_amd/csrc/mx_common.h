@@ -128,6 +128,17 @@ __device__ __forceinline__ f4_t mfma_mx(u4_t w, uint32_t wscale, i8_t x, uint32_
                                                           (int)xscale);
 }
 
+// Consecutive tiles on one XCD (round-robin dispatch), whatever their number.
+__device__ __forceinline__ int xcd_run(int b, int nb) {
+  const int x = b & 7, q = nb >> 3, rem = nb & 7;
+  return x * q + min(x, rem) + (b >> 3);
+}
+
+// 16 bytes per lane from global memory straight to LDS (dst + 16 lane)
+__device__ __forceinline__ void dma_lds(__amdgpu_buffer_rsrc_t r, void* dst, uint32_t off, uint32_t soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 16, off, soff, 0, 0);
+}
+
 // 8 outputs of a lane in 16 bits, or quantized into X's format (the block's four
 // lanes are 16 apart). n: the first output; rows past M write nothing.
 template <int DT, int FMT, bool QUANT>

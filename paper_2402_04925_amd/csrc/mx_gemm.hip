@@ -17,18 +17,23 @@
 namespace tpdq {
 namespace {
 
-// Few rows of X: the weight stream bounds it. A workgroup owns NP tiles of 32
-// outputs (GATED: of the gate and the up projection) over the whole of K and MT
-// tiles of 16 rows; its waves take chunks of 512 elements of K in turn, the
-// weights of a chunk straight to registers (1 KB contiguous per load), and add
-// their accumulators in LDS at the end.
-template <int DT, int FMT, int MT, int NP, bool GATED, bool QUANT, int NWMAX>
+// Few rows of X: the weight stream bounds it. A workgroup owns TN operands of 16
+// outputs (2: a whole tile; GATED: of the gate and the up projection) over the
+// whole of K and MT tiles of 16 rows. Its waves take chunks of 512 elements of K in
+// turn: the chunk's weights straight to registers (1 KB contiguous per load), its
+// rows of X to a part of LDS of the wave's own, 8 rows of a 128-byte line per load
+// and read back as the operand (a load of the operand itself would touch 16 rows
+// of half a line). The waves add their accumulators in LDS at the end.
+template <int DT, int FMT, int MT, int TN, bool GATED, bool QUANT, int NWMAX>
 __global__ __launch_bounds__(NWMAX * 64) void k_mx_rows(MxArgs a) {
+  static_assert(TN == 2 || (!GATED && !QUANT), "a block of outputs is a whole tile");
   constexpr int P = GATED ? 2 : 1;
-  constexpr int NT = NP * P * 2;  // operands (16 outputs) per workgroup
-  constexpr int XW = FMT == kFp4 ? 1 : 2;  // 16-byte loads of X per step
+  constexpr int NT = TN * P;                 // operands per workgroup
+  constexpr int XW = FMT == kFp4 ? 1 : 2;    // 64-byte halves of a row's line per step
+  constexpr int LINES = 2 * XW;              // 128-byte lines of a row per chunk
+  constexpr int XWAVE = MT * LINES * 2048;   // LDS of a wave
   extern __shared__ __align__(16) unsigned char smem[];
-  f4_t* red = (f4_t*)smem;  // [wave][MT * NT][64]
+  f4_t* red = (f4_t*)smem;  // [wave][MT * NT][64], after the loop
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nw = blockDim.x >> 6;
@@ -36,28 +41,30 @@ __global__ __launch_bounds__(NWMAX * 64) void k_mx_rows(MxArgs a) {
   const int steps = (a.K + kMxStep - 1) / kMxStep;
   const int chunks = (a.K + kMxChunk - 1) / kMxChunk;
   const int tiles = (a.N + kMxTile - 1) / kMxTile;
-  const int T0 = xcd_tile(blockIdx.x, gridDim.x) * NP;
-  const int m0 = blockIdx.y * 16 * MT;
+  const int wg = xcd_run(blockIdx.x, gridDim.x);
+  const int T = TN == 2 ? wg : wg >> 1;      // the tile, and of half a tile the operand
+  const int j0 = TN == 2 ? 0 : wg & 1;
+  unsigned char* xl = smem + wave * XWAVE;
 
-  // tiles past the last one and rows past M load zeros from the resource bounds
+  // a tile past the last one and rows past M load zeros from the resource bounds
   const uint32_t wbytes = (uint32_t)(tiles - 1) * (uint32_t)a.ldwc + (uint32_t)steps * 2048u;
   const uint32_t sbytes = (uint32_t)(tiles - 1) * (uint32_t)a.ldws + (uint32_t)chunks * 512u;
   const uint32_t xbytes = (uint32_t)(a.M - 1) * (uint32_t)a.x.ld_c + (uint32_t)steps * (64u * XW);
   const uint32_t xsbytes = (uint32_t)(a.M - 1) * (uint32_t)a.x.ld_s + (uint32_t)chunks * 16u;
-  const __amdgpu_buffer_rsrc_t rx = buffer_rsrc(a.x.codes, xbytes), rxs = buffer_rsrc(a.x.scales, xsbytes);
-  uint32_t offx[MT], offxs[MT];
+  const __amdgpu_buffer_rsrc_t rxs = buffer_rsrc(a.x.scales, xsbytes);
+  uint32_t offx[2 * MT], offxs[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int m = m0 + 16 * t + r;
-    offx[t] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 16u * g : kOutOfRange;
-    offxs[t] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_s : kOutOfRange;
+  for (int t = 0; t < 2 * MT; ++t) {  // 8 rows each; lane: row lane / 8, chunk of 16 bytes swapped as in LDS
+    const int m = 8 * t + (lane >> 3);
+    offx[t] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 16u * (uint32_t)((lane & 7) ^ (4 * (t & 1) + (lane >> 4)))
+                      : kOutOfRange;
   }
-  uint32_t offw[NP], offs[NP];
 #pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    offw[p] = T0 + p < tiles ? (uint32_t)(T0 + p) * (uint32_t)a.ldwc + 16u * lane : kOutOfRange;
-    offs[p] = T0 + p < tiles ? (uint32_t)(T0 + p) * (uint32_t)a.ldws + 8u * lane : kOutOfRange;
-  }
+  for (int t = 0; t < MT; ++t) offxs[t] = 16 * t + r < a.M ? (uint32_t)(16 * t + r) * (uint32_t)a.x.ld_s : kOutOfRange;
+  const uint32_t offw = T < tiles ? (uint32_t)T * (uint32_t)a.ldwc + 1024u * j0 + 16u * lane : kOutOfRange;
+  const uint32_t offs = T < tiles ? (uint32_t)T * (uint32_t)a.ldws + 8u * lane : kOutOfRange;
+  // row r's chunk c of a line is at place c ^ (r / 2): the 16 rows in all 64 banks
+  const int xpos0 = r * 128 + ((g ^ (r >> 1)) << 4), xpos1 = xpos0 ^ 64;
 
   f4_t acc[MT][NT];
 #pragma unroll
@@ -65,56 +72,69 @@ __global__ __launch_bounds__(NWMAX * 64) void k_mx_rows(MxArgs a) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) acc[t][i] = f4_t{0.f, 0.f, 0.f, 0.f};
 
+#pragma unroll 1
   for (int c = wave; c < chunks; c += nw) {
-    u4_t w[NT][4];
-    u2_t ws[NT / 2];
+#pragma unroll
+    for (int l = 0; l < LINES; ++l) {
+      const bool in = 4 * c + 2 * l / XW < steps;
+      const __amdgpu_buffer_rsrc_t rx = buffer_rsrc(a.x.codes, in ? xbytes : 0u);
+#pragma unroll
+      for (int t = 0; t < 2 * MT; ++t)
+        if (8 * t < a.M)  // rows past M only reach outputs past M: their place may hold anything
+          dma_lds(rx, xl + ((t >> 1) * LINES + l) * 2048 + (t & 1) * 1024, offx[t],
+                  in ? (uint32_t)(c * LINES + l) * 128u : 0u);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     u4_t xs[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) xs[t] = buffer_load16(rxs, offxs[t] + 16u * c);
+    u2_t ws[P];
+    u4_t w[NT][4];
 #pragma unroll
     for (int h = 0; h < P; ++h) {
-      const __amdgpu_buffer_rsrc_t rw = buffer_rsrc(h ? a.wc_up : a.wc, wbytes);
       const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(h ? a.ws_up : a.ws, sbytes);
+      ws[h] = __builtin_bit_cast(u2_t, __builtin_amdgcn_raw_buffer_load_b64(rs, offs + 512u * c, 0, 0));
+    }
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        ws[h * NP + p] = __builtin_bit_cast(u2_t, __builtin_amdgcn_raw_buffer_load_b64(rs, offs[p] + 512u * c, 0, 0));
+    for (int s = 0; s < 4; ++s) {
+      const bool in = 4 * c + s < steps;
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            w[(h * NP + p) * 2 + j][s] = buffer_load16<kNonTemporal>(
-                rw, 4 * c + s < steps ? offw[p] + (uint32_t)(4 * c + s) * 2048u + 1024u * j : kOutOfRange);
+      for (int i = 0; i < NT; ++i) {
+        const __amdgpu_buffer_rsrc_t rw = buffer_rsrc(GATED && i >= 2 ? a.wc_up : a.wc, in ? wbytes : 0u);
+        w[i][s] = __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(
+            rw, offw + 1024u * (i & 1), in ? (uint32_t)(4 * c + s) * 2048u : 0u, kNonTemporal));
       }
     }
-    i8_t x[MT][4];
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const bool in = 4 * c + s < steps;
-        const uint32_t o = offx[t] + (uint32_t)(4 * c + s) * (64u * XW);
-        const u4_t lo = buffer_load16(rx, in ? o : kOutOfRange);
-        u4_t hi = {0u, 0u, 0u, 0u};
-        if constexpr (XW == 2) hi = buffer_load16(rx, in ? o + 64u : kOutOfRange);
-        x[t][s] = i8_t{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-      }
+    // X has landed, the loads issued after it may be in flight
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(MT + P + 4 * NT) : "memory");
     auto step = [&](auto sel) {
       constexpr int s = decltype(sel)::value;
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
+        const unsigned char* xt = xl + (t * LINES + s * XW / 2) * 2048;
+        const u4_t lo = *(const u4_t*)(xt + (XW == 1 && s % 2 ? xpos1 : xpos0));
+        u4_t hi = {0u, 0u, 0u, 0u};
+        if constexpr (XW == 2) hi = *(const u4_t*)(xt + xpos1);
+        const i8_t x = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         const uint32_t xsc = xs[t][s] >> (8 * g);
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-          acc[t][i] = mfma_mx<FMT, s>(w[i][s], ws[i >> 1][i & 1], x[t][s], xsc, acc[t][i]);
+        for (int i = 0; i < NT; ++i) {
+          const uint32_t wsc = TN == 2 ? ws[i >> 1][i & 1] : (j0 ? ws[0].y : ws[0].x);
+          acc[t][i] = mfma_mx<FMT, s>(w[i][s], wsc, x, xsc, acc[t][i]);
+        }
       }
     };
     step(std::integral_constant<int, 0>{});
     step(std::integral_constant<int, 1>{});
     step(std::integral_constant<int, 2>{});
     step(std::integral_constant<int, 3>{});
+    // the next chunk's loads overwrite what was read here
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
+  __syncthreads();
 
-  // acc of operand i of tile pair (h, p), j = i % 2, row tile t -> red
+  // operand i of row tile t -> red
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -127,55 +147,65 @@ __global__ __launch_bounds__(NWMAX * 64) void k_mx_rows(MxArgs a) {
     red[i] = s;
   }
   __syncthreads();
-  for (int i = wave; i < MT * NP; i += nw) {
-    const int t = i / NP, p = i - t * NP;
-    float v[8];
+  for (int t = wave; t < MT; t += nw) {
+    const int m = 16 * t + r;
+    if constexpr (TN == 1) {
+      const f4_t y = red[t * 64 + lane];
+      const int64_t n = (int64_t)T * kMxTile + 8 * g + 4 * j0;
+      if (m < a.M && n < a.N) *(u2_t*)(a.Y + (int64_t)m * a.ldy + n) = u2_t{pack2<DT>(y[0], y[1]), pack2<DT>(y[2], y[3])};
+    } else {
+      float v[8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const f4_t y = red[(t * NT + 2 * p + j) * 64 + lane];
-      f4_t u = y;
-      if constexpr (GATED) u = red[(t * NT + 2 * (NP + p) + j) * 64 + lane];
+      for (int j = 0; j < 2; ++j) {
+        const f4_t y = red[(t * NT + j) * 64 + lane];
+        f4_t u = y;
+        if constexpr (GATED) u = red[(t * NT + 2 + j) * 64 + lane];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * j + e] = GATED ? silu_mul(y[e], u[e]) : y[e];
+        for (int e = 0; e < 4; ++e) v[4 * j + e] = GATED ? silu_mul(y[e], u[e]) : y[e];
+      }
+      store_out8<DT, FMT, QUANT>(a, v, m, (int64_t)T * kMxTile + 8 * g);
     }
-    store_out8<DT, FMT, QUANT>(a, v, m0 + 16 * t + r, (int64_t)(T0 + p) * kMxTile + 8 * g);
   }
 }
 
-template <int DT, int FMT, int MT, int NP, bool GATED, bool QUANT, int NWMAX>
+template <int DT, int FMT, int MT, int TN, bool GATED, bool QUANT, int NWMAX>
 hipError_t rows_launch(const MxArgs& a, hipStream_t s) {
   // quantized outputs: also the tiles of the padding to whole chunks (zeros)
   const int tiles = (int)(QUANT ? mx_chunks(a.N) * (kMxChunk / kMxTile) : (a.N + kMxTile - 1) / kMxTile);
   const int nw = (int)std::min<int64_t>(NWMAX, mx_chunks(a.K));
-  const size_t lds = (size_t)nw * MT * NP * (GATED ? 4 : 2) * 1024;
-  auto* k = k_mx_rows<DT, FMT, MT, NP, GATED, QUANT, NWMAX>;
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  constexpr int x = MT * (FMT == kFp4 ? 2 : 4) * 2048, red = MT * TN * (GATED ? 2 : 1) * 1024;
+  constexpr int wave_lds = x > red ? x : red;
+  static_assert((size_t)NWMAX * wave_lds <= kLdsMax, "");
+  auto* k = k_mx_rows<DT, FMT, MT, TN, GATED, QUANT, NWMAX>;
+  if (NWMAX * wave_lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, NWMAX * wave_lds);
     if (e != hipSuccess) return e;
   }
-  const int row_groups = (a.M + 16 * MT - 1) / (16 * MT);
-  k<<<dim3((unsigned)((tiles + NP - 1) / NP), (unsigned)row_groups), dim3((unsigned)nw * 64), lds, s>>>(a);
+  k<<<dim3((unsigned)(TN == 2 ? tiles : 2 * tiles)), dim3((unsigned)nw * 64), nw * wave_lds, s>>>(a);
   return hipGetLastError();
 }
 
 template <int DT, int FMT, bool GATED, bool QUANT>
-hipError_t rows_pick(const MxArgs& a, hipStream_t s) {
-  if (a.M <= 16) return rows_launch<DT, FMT, 1, 1, GATED, QUANT, 16>(a, s);
-  if (a.M <= 32) return rows_launch<DT, FMT, 2, 1, GATED, QUANT, 8>(a, s);
-  return rows_launch<DT, FMT, 4, 1, GATED, QUANT, 8>(a, s);
+hipError_t rows_pick(const MxArgs& a, int bm, hipStream_t s) {
+  if constexpr (!GATED && !QUANT) {
+    if (bm == -1 && a.M <= 16) return rows_launch<DT, FMT, 1, 1, GATED, QUANT, 16>(a, s);
+    if (bm == -1) return rows_launch<DT, FMT, 2, 1, GATED, QUANT, 8>(a, s);
+  }
+  if (a.M <= 16) return rows_launch<DT, FMT, 1, 2, GATED, QUANT, 16>(a, s);
+  return rows_launch<DT, FMT, 2, 2, GATED, QUANT, 8>(a, s);
 }
 
 template <int FMT>
-hipError_t rows_of(const MxArgs& a, int dt, hipStream_t s) {
-  if (a.wc_up) return rows_pick<kF16, FMT, true, true>(a, s);
-  if (!a.Y) return rows_pick<kF16, FMT, false, true>(a, s);
-  return dt == TPDQ_BF16 ? rows_pick<kBF16, FMT, false, false>(a, s) : rows_pick<kF16, FMT, false, false>(a, s);
+hipError_t rows_of(const MxArgs& a, int bm, int dt, hipStream_t s) {
+  if (a.wc_up) return rows_pick<kF16, FMT, true, true>(a, bm, s);
+  if (!a.Y) return rows_pick<kF16, FMT, false, true>(a, bm, s);
+  return dt == TPDQ_BF16 ? rows_pick<kBF16, FMT, false, false>(a, bm, s) : rows_pick<kF16, FMT, false, false>(a, bm, s);
 }
 
 }  // namespace
 
 MxPlan plan_mx(int M, int N, int K, int fmt, bool gated) {
-  if (M <= 64) return MxPlan{0, 1};
+  if (M <= 32) return MxPlan{0, 1};
   return MxPlan{M <= 128 ? 3 : 2, 1};
 }
 
@@ -187,8 +217,8 @@ hipError_t launch_mx_gemm(MxArgs a, int dt, int fmt, float* part, hipStream_t s)
   const MxPlan p = plan_mx(a.M, a.N, a.K, fmt, a.wc_up != nullptr);
   a.ks = p.ks;
   a.part = part;
-  if (p.bm) return launch_mx_tiles(a, p.bm, dt, fmt, s);
-  return fmt == TPDQ_MX_FP4 ? rows_of<kFp4>(a, dt, s) : rows_of<kFp8>(a, dt, s);
+  if (p.bm > 0) return launch_mx_tiles(a, p.bm, dt, fmt, s);
+  return fmt == TPDQ_MX_FP4 ? rows_of<kFp4>(a, p.bm, dt, s) : rows_of<kFp8>(a, p.bm, dt, s);
 }
 
 }  // namespace tpdq

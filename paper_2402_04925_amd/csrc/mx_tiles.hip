@@ -19,17 +19,6 @@
 namespace tpdq {
 namespace {
 
-// Consecutive tiles on one XCD (round-robin dispatch), whatever their number.
-__device__ __forceinline__ int xcd_run(int b, int nb) {
-  const int x = b & 7, q = nb >> 3, rem = nb & 7;
-  return x * q + min(x, rem) + (b >> 3);
-}
-
-// 16 bytes per lane from global memory straight to LDS (dst + 16 lane)
-__device__ __forceinline__ void dma_lds(__amdgpu_buffer_rsrc_t r, void* dst, uint32_t off, uint32_t soff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 16, off, soff, 0, 0);
-}
-
 template <int DT, int FMT, int RT, int WM, int NP, int NW, int S, bool GATED, bool QUANT>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_mx_tiles(MxArgs a) {
   static_assert(!GATED || NP == 2, "a tile of the gate and one of the up projection");
