@@ -93,10 +93,10 @@ size_t y1_codes_bytes(int64_t M, int64_t N) { return align_up((size_t)(M * mx_ro
 size_t y1_bytes(int64_t M, int64_t N) { return y1_codes_bytes(M, N) + align_up((size_t)(M * mx_row_scales(N))); }
 
 // split-K parts of one product, for the format of X that takes more
-size_t part_bytes(int M, int N, int K, bool gated) {
+size_t part_bytes(int M, int N, int K, bool gated, bool quant) {
   size_t most = 0;
   for (int fmt : {(int)TPDQ_MX_FP4, (int)TPDQ_MX_FP8})
-    most = std::max(most, mx_part_bytes(plan_mx(M, N, K, fmt, gated), M, N, gated));
+    most = std::max(most, mx_part_bytes(plan_mx(M, N, K, fmt, gated, quant), M, N, gated));
   return most;
 }
 
@@ -108,11 +108,11 @@ extern "C" {
 
 size_t tpdq_mx_workspace_bytes(int op, int32_t M, const tpdq_mx* a, const tpdq_mx* b) {
   if (M < 1 || !valid_size(a)) return 0;
-  if (op == 0) return part_bytes(M, a->R, a->K, false);
+  if (op == 0) return part_bytes(M, a->R, a->K, false, false);
   if (op != 1 || !valid_size(b) || b->K != a->R) return 0;
   // Y1, then the parts of the product at hand (the first may be gated or not)
-  return y1_bytes(M, a->R) + std::max({part_bytes(M, a->R, a->K, true), part_bytes(M, a->R, a->K, false),
-                                       part_bytes(M, b->R, b->K, false)});
+  return y1_bytes(M, a->R) + std::max({part_bytes(M, a->R, a->K, true, true), part_bytes(M, a->R, a->K, false, true),
+                                       part_bytes(M, b->R, b->K, false, false)});
 }
 
 tpdq_status tpdq_mx_quantize(const void* X, int64_t ldx, tpdq_dtype dtype, const tpdq_mx* q, void* stream) {

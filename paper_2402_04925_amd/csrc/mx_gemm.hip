@@ -186,27 +186,101 @@ hipError_t rows_launch(const MxArgs& a, hipStream_t s) {
 }
 
 template <int DT, int FMT, bool GATED, bool QUANT>
-hipError_t rows_pick(const MxArgs& a, int bm, hipStream_t s) {
+hipError_t rows_pick(const MxArgs& a, int kind, hipStream_t s) {
+  constexpr int NW4 = FMT == kFp4 ? 10 : 5;  // what LDS holds of 64 rows
   if constexpr (!GATED && !QUANT) {
-    if (bm == -1 && a.M <= 16) return rows_launch<DT, FMT, 1, 1, GATED, QUANT, 16>(a, s);
-    if (bm == -1) return rows_launch<DT, FMT, 2, 1, GATED, QUANT, 8>(a, s);
+    if (kind == kMxRowsHalf) {
+      if (a.M <= 16) return rows_launch<DT, FMT, 1, 1, GATED, QUANT, 16>(a, s);
+      if (a.M <= 32) return rows_launch<DT, FMT, 2, 1, GATED, QUANT, 8>(a, s);
+      return rows_launch<DT, FMT, 4, 1, GATED, QUANT, NW4>(a, s);
+    }
   }
   if (a.M <= 16) return rows_launch<DT, FMT, 1, 2, GATED, QUANT, 16>(a, s);
-  return rows_launch<DT, FMT, 2, 2, GATED, QUANT, 8>(a, s);
+  if (a.M <= 32) return rows_launch<DT, FMT, 2, 2, GATED, QUANT, 8>(a, s);
+  return rows_launch<DT, FMT, 4, 2, GATED, QUANT, NW4>(a, s);
 }
 
 template <int FMT>
-hipError_t rows_of(const MxArgs& a, int bm, int dt, hipStream_t s) {
-  if (a.wc_up) return rows_pick<kF16, FMT, true, true>(a, bm, s);
-  if (!a.Y) return rows_pick<kF16, FMT, false, true>(a, bm, s);
-  return dt == TPDQ_BF16 ? rows_pick<kBF16, FMT, false, false>(a, bm, s) : rows_pick<kF16, FMT, false, false>(a, bm, s);
+hipError_t rows_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
+  if (a.wc_up) return rows_pick<kF16, FMT, true, true>(a, kind, s);
+  if (!a.Y) return rows_pick<kF16, FMT, false, true>(a, kind, s);
+  return dt == TPDQ_BF16 ? rows_pick<kBF16, FMT, false, false>(a, kind, s) : rows_pick<kF16, FMT, false, false>(a, kind, s);
 }
 
 }  // namespace
 
-MxPlan plan_mx(int M, int N, int K, int fmt, bool gated) {
-  if (M <= 32) return MxPlan{0, 1};
-  return MxPlan{M <= 128 ? 3 : 2, 1};
+// Microseconds of a product, fitted to 7,000 launches on 400 random sizes (1 to 2048
+// rows, 512 to 32768 outputs, 512 to 16384 of K; 7 to 15% rms): the choice made by
+// them is 1.6% slower than the best of all kernels, tiles and splits on average, 25%
+// at worst. A workgroup takes max(c1, c2 n) per step of K, n workgroups to a CU, e
+// more for each beyond the first; parts are written and read once. What it is for:
+// 8192 x 8192 at 64 rows fp8 takes 16.0 us in the few-row kernel, 16.4 in tiles of 64
+// x 128 over 4 splits and 23 without; 8192 x 28672 53, 37 and 30; 3584 of K x 8192 at
+// 256 rows 11.3 in tiles of 64 x 128, 15.2 of 64 x 256; 14336 x 8192 at 2048 rows 281
+// and 202, but 194 of 128 x 512.
+struct TileCost {
+  int kind, bm, bn;
+  double start, c1, c2, e, reduce, mb;
+};
+constexpr TileCost kTileFp8[] = {
+    {kMxTiles128x512, 128, 512, 7.3, 0.00, 1.38, 3.9, 6.8, 8.3e6}, {kMxTiles64x512, 64, 512, 4.8, 0.13, 0.67, 2.8, 3.9, 5.4e6},
+    {kMxTiles64x256, 64, 256, 4.4, 0.00, 0.374, 1.3, 3.4, 5.0e6},  {kMxTiles128x256, 128, 256, 5.3, 0.20, 0.67, 1.6, 4.6, 6.3e6},
+    {kMxTiles64x128, 64, 128, 3.7, 0.08, 0.238, 0.9, 3.2, 4.7e6}};
+constexpr TileCost kTileFp4[] = {
+    {kMxTiles128x512, 128, 512, 7.8, 0.16, 0.70, 7.0, 6.7, 8.2e6}, {kMxTiles64x512, 64, 512, 4.2, 0.02, 0.535, 2.7, 4.3, 5.6e6},
+    {kMxTiles64x256, 64, 256, 4.0, 0.15, 0.266, 2.0, 3.6, 5.1e6},  {kMxTiles128x256, 128, 256, 5.7, 0.20, 0.42, 2.1, 4.7, 6.6e6},
+    {kMxTiles64x128, 64, 128, 3.4, 0.09, 0.165, 0.9, 3.3, 4.3e6}};
+// The few-row kernel: start + n (workgroups to a CU) iter (chunks a wave takes) +
+// wave (waves), by rows up to 16, 32, 64
+struct RowsCost {
+  int waves;
+  double start, iter, wave;
+};
+constexpr RowsCost kRowsFp8[] = {{16, 2.2, 0.73, 0.24}, {8, 0.8, 2.24, 0.38}, {5, 0.8, 3.5, 0.42}};
+constexpr RowsCost kRowsFp4[] = {{16, 2.2, 0.64, 0.22}, {8, 2.0, 1.41, 0.23}, {10, 2.4, 1.23, 0.49}};
+constexpr int kCus = 256;
+// split-K parts of a call take at most this much workspace
+constexpr int64_t kMxPartBytes = (int64_t)64 << 20;
+
+int up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+MxPlan plan_mx(int M, int N, int K, int fmt, bool gated, bool quant) {
+  const bool fp4 = fmt == TPDQ_MX_FP4;
+  const int weights = gated ? 2 : 1;
+  const int steps = (int)mx_steps(K), chunks = (int)mx_chunks(K), tiles = up(N, kMxTile);
+  MxPlan best{kMxRows, 1};
+  double least = 1e30;
+  if (M <= 64) {
+    const RowsCost& c = (fp4 ? kRowsFp4 : kRowsFp8)[M <= 16 ? 0 : M <= 32 ? 1 : 2];
+    const int waves = std::min(c.waves, chunks);
+    least = c.start + up(tiles, kCus) * weights * c.iter * up(chunks, waves) + c.wave * waves;
+    // Half tiles where they all find a CU of their own: 8192 x 3584 at 1 row 6.7 ->
+    // 5.7 us, at 16 8.1 -> 7.1; past that they are slower (6144 x 6144 at 16 rows,
+    // 192 tiles: 7.3 -> 9.8). A block of quantized outputs is a whole tile.
+    if (!quant && 2 * tiles <= kCus) {
+      best.kind = kMxRowsHalf;
+      least *= 0.85;
+    }
+  }
+  for (const TileCost& c : fp4 ? kTileFp4 : kTileFp8) {
+    // the gated product has a tile of each projection per wave; 128 rows with half
+    // of them empty never pay
+    if (gated && (c.kind == kMxTiles64x128 || c.kind == kMxTiles128x256)) continue;
+    if (c.bm > 64 && M <= 64) continue;
+    const int64_t wgs = (int64_t)up(M, c.bm) * up((int64_t)N * weights, c.bn);
+    const int block = !fp4 && c.kind == kMxTiles128x512 ? 2 : 4, blocks = up(steps, block);
+    for (int ks : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+      if (ks > blocks || (ks > 1 && (wgs * ks > 3 * kCus || (int64_t)ks * M * N * 4 * weights > kMxPartBytes))) break;
+      const int n = up(wgs * ks, kCus);
+      double t = c.start + (double)(up(blocks, ks) * block) * std::max(c.c1, c.c2 * n) + c.e * (n - 1);
+      if (ks > 1) t += c.reduce + (double)ks * M * N * weights * 8 / c.mb;
+      if (t < least) {
+        least = t;
+        best = MxPlan{c.kind, ks};
+      }
+    }
+  }
+  return best;
 }
 
 size_t mx_part_bytes(const MxPlan& p, int M, int N, bool gated) {
@@ -214,11 +288,11 @@ size_t mx_part_bytes(const MxPlan& p, int M, int N, bool gated) {
 }
 
 hipError_t launch_mx_gemm(MxArgs a, int dt, int fmt, float* part, hipStream_t s) {
-  const MxPlan p = plan_mx(a.M, a.N, a.K, fmt, a.wc_up != nullptr);
+  const MxPlan p = plan_mx(a.M, a.N, a.K, fmt, a.wc_up != nullptr, a.Y == nullptr);
   a.ks = p.ks;
   a.part = part;
-  if (p.bm > 0) return launch_mx_tiles(a, p.bm, dt, fmt, s);
-  return fmt == TPDQ_MX_FP4 ? rows_of<kFp4>(a, p.bm, dt, s) : rows_of<kFp8>(a, p.bm, dt, s);
+  if (p.kind != kMxRows && p.kind != kMxRowsHalf) return launch_mx_tiles(a, p.kind, dt, fmt, s);
+  return fmt == TPDQ_MX_FP4 ? rows_of<kFp4>(a, p.kind, dt, s) : rows_of<kFp8>(a, p.kind, dt, s);
 }
 
 }  // namespace tpdq

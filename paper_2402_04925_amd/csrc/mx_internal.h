@@ -74,16 +74,17 @@ struct MxArgs {
   float* part;  // ks > 1: [ks][(gate, up)][M][N]
   int ks;       // K splits (tiles kernel)
 };
-// How a product runs: bm = 0 the few-row kernel, else tiles of bm (64, 128 or 256)
-// rows with K split over ks workgroups (fp32 parts, added in the splits' order by a
-// second kernel).
+// How a product runs: the few-row kernel over whole or half tiles of 32 outputs, or
+// tiles of rows x weight rows (gated: half of them of each projection) with K split
+// over ks workgroups (fp32 parts, added in the splits' order by a second kernel).
+enum MxKind { kMxRows, kMxRowsHalf, kMxTiles128x512, kMxTiles64x512, kMxTiles64x256, kMxTiles128x256, kMxTiles64x128 };
 struct MxPlan {
-  int bm, ks;
+  int kind, ks;
 };
-MxPlan plan_mx(int M, int N, int K, int fmt, bool gated);
+MxPlan plan_mx(int M, int N, int K, int fmt, bool gated, bool quant);
 size_t mx_part_bytes(const MxPlan& p, int M, int N, bool gated);
 // part: mx_part_bytes of the plan
 hipError_t launch_mx_gemm(MxArgs a, int dt, int fmt, float* part, hipStream_t s);
-hipError_t launch_mx_tiles(const MxArgs& a, int bm, int dt, int fmt, hipStream_t s);  // mx_tiles.hip
+hipError_t launch_mx_tiles(const MxArgs& a, int kind, int dt, int fmt, hipStream_t s);  // mx_tiles.hip
 
 }  // namespace tpdq

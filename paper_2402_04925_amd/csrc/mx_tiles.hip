@@ -273,19 +273,17 @@ hipError_t tiles_launch(const MxArgs& a, hipStream_t s) {
 }
 
 template <int DT, int FMT, bool GATED, bool QUANT>
-hipError_t tiles_pick(const MxArgs& a, int bm, hipStream_t s) {
-  constexpr int S2 = FMT == kFp4 ? 4 : 2;
-  switch (bm) {
-    case 1: return tiles_launch<DT, FMT, 8, 2, 2, 8, S2, GATED, QUANT>(a, s);
-    case 2: return tiles_launch<DT, FMT, 8, 1, 2, 8, S2, GATED, QUANT>(a, s);
-    case 3: return tiles_launch<DT, FMT, 4, 1, 2, 8, 4, GATED, QUANT>(a, s);
-    case 4: return tiles_launch<DT, FMT, 4, 1, 2, 4, 4, GATED, QUANT>(a, s);
-    case 5: return tiles_launch<DT, FMT, 4, 2, 2, 8, 4, GATED, QUANT>(a, s);
+hipError_t tiles_pick(const MxArgs& a, int kind, hipStream_t s) {
+  constexpr int S2 = FMT == kFp4 ? 4 : 2;  // fp8 at 128 x 512: registers for two steps
+  switch (kind) {
+    case kMxTiles128x512: return tiles_launch<DT, FMT, 8, 1, 2, 8, S2, GATED, QUANT>(a, s);
+    case kMxTiles64x512: return tiles_launch<DT, FMT, 4, 1, 2, 8, 4, GATED, QUANT>(a, s);
+    case kMxTiles64x256: return tiles_launch<DT, FMT, 4, 1, 2, 4, 4, GATED, QUANT>(a, s);
   }
   if constexpr (!GATED) {
-    switch (bm) {
-      case 7: return tiles_launch<DT, FMT, 4, 1, 1, 4, 4, GATED, QUANT>(a, s);
-      case 6: return tiles_launch<DT, FMT, 8, 1, 1, 8, 4, GATED, QUANT>(a, s);
+    switch (kind) {
+      case kMxTiles128x256: return tiles_launch<DT, FMT, 8, 1, 1, 8, 4, GATED, QUANT>(a, s);
+      case kMxTiles64x128: return tiles_launch<DT, FMT, 4, 1, 1, 4, 4, GATED, QUANT>(a, s);
     }
   }
   return hipErrorInvalidValue;
@@ -294,16 +292,16 @@ hipError_t tiles_pick(const MxArgs& a, int bm, hipStream_t s) {
 // Outputs in 16 bits, or quantized (the gated product always is: the MLP's first
 // half), which no element type enters.
 template <int FMT>
-hipError_t tiles_of(const MxArgs& a, int bm, int dt, hipStream_t s) {
-  if (a.wc_up) return tiles_pick<kF16, FMT, true, true>(a, bm, s);
-  if (!a.Y) return tiles_pick<kF16, FMT, false, true>(a, bm, s);
-  return dt == TPDQ_BF16 ? tiles_pick<kBF16, FMT, false, false>(a, bm, s) : tiles_pick<kF16, FMT, false, false>(a, bm, s);
+hipError_t tiles_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
+  if (a.wc_up) return tiles_pick<kF16, FMT, true, true>(a, kind, s);
+  if (!a.Y) return tiles_pick<kF16, FMT, false, true>(a, kind, s);
+  return dt == TPDQ_BF16 ? tiles_pick<kBF16, FMT, false, false>(a, kind, s) : tiles_pick<kF16, FMT, false, false>(a, kind, s);
 }
 
 }  // namespace
 
-hipError_t launch_mx_tiles(const MxArgs& a, int bm, int dt, int fmt, hipStream_t s) {
-  return fmt == TPDQ_MX_FP4 ? tiles_of<kFp4>(a, bm, dt, s) : tiles_of<kFp8>(a, bm, dt, s);
+hipError_t launch_mx_tiles(const MxArgs& a, int kind, int dt, int fmt, hipStream_t s) {
+  return fmt == TPDQ_MX_FP4 ? tiles_of<kFp4>(a, kind, dt, s) : tiles_of<kFp8>(a, kind, dt, s);
 }
 
 }  // namespace tpdq
