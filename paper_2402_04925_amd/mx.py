@@ -8,7 +8,7 @@ torch's allocator within the call, on the device's current stream.
 from __future__ import annotations
 
 import ctypes
-import dataclasses
+import functools
 from typing import Optional
 
 from . import _abi
@@ -22,74 +22,98 @@ def _up(a: int, b: int) -> int:
     return -(-a // b)
 
 
-def _on(device):
-    """Makes the tensors' device current for the launch where it is not."""
+def _run(device, f, *args):
+    """f(*args, stream) with the tensors' device current (a launch needs that)."""
     torch = _torch()
     if device.index is None or device.index == torch.cuda.current_device():
-        return None
-    return torch.cuda.device(device)
-
-
-def _run(device, f, *args):
-    guard = _on(device)
-    if guard is None:
-        _abi.check(f(*args, _stream_handle(device)))
+        st = f(*args, _stream_handle(device))
     else:
-        with guard:
-            _abi.check(f(*args, _stream_handle(device)))
+        with torch.cuda.device(device):
+            st = f(*args, _stream_handle(device))
+    if st:
+        _abi.check(st)
 
 
-def _gpu(t, name):
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must be on a GPU, got {t.device}")
+def _device_of(name, t):
+    dev = t.device
+    if dev.type != "cuda":
+        raise ValueError(f"{name} must be on a GPU, got {dev}")
+    return dev
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, X on {device}")
+def _same_device(device, name, t):
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, X on {device}")
 
 
-def _rows16(name, t, shape=None, dtype=None):
-    """A 16-bit matrix with unit column stride (of this shape and type)."""
+def _rows16(name, t, M=None, K=None, dtype=None):
+    """A 16-bit matrix with unit column stride (M x K, of dtype)."""
     if t.dim() != 2 or t.stride(1) != 1:
         raise ValueError(f"{name} must be 2-D with unit column stride")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if M is not None and (t.shape[0] != M or t.shape[1] != K):
+        raise ValueError(f"{name} must be [{M}][{K}], got {list(t.shape)}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
 
 
-@dataclasses.dataclass
 class MxTensor:
     """An R x K tensor of MX numbers in device memory (or a shard of one as views).
+    Its fields are not assigned anew: the C struct that calls pass is made once.
 
     MX_ROWS: codes [R][>= padded K], float8_e4m3fn (fp8) or uint8 with two codes
-    to a byte (fp4); scale_bytes uint8 [R][>= padded blocks]. MX_TILED (weights):
-    codes uint8 [ceil(R/32)][...], scale_bytes uint8 [ceil(R/32)][...], the order that
-    mx_gemm reads (see include/tpdq.h). Rows are padded to whole steps (codes, 128
-    elements) and chunks (scales, 512 elements), with zeros."""
-    codes: object
-    scale_bytes: object
-    R: int
-    K: int
-    fmt: int
-    layout: int = MX_ROWS
+    to a byte (fp4); padded_scales float8_e8m0fnu [R][>= padded blocks]. MX_TILED
+    (weights): codes uint8 [ceil(R/32)][...], padded_scales [ceil(R/32)][...], the order
+    that mx_gemm reads (see include/tpdq.h). Rows are padded to whole steps (codes,
+    128 elements) and chunks (scales, 512 elements), with zero bytes."""
+
+    __slots__ = ("_codes", "_scales", "_R", "_K", "_fmt", "_layout", "_device", "_c", "_ref")
+
+    def __init__(self, codes, padded_scales, R: int, K: int, fmt: int, layout: int = MX_ROWS):
+        torch = _torch()
+        c, s = codes, padded_scales
+        rows = R if layout == MX_ROWS else _up(R, _TILE)
+        dev = c.device
+        if (c.dim() != 2 or s.dim() != 2 or c.stride(1) != 1 or s.stride(1) != 1 or s.device != dev
+                or c.dtype is not (torch.float8_e4m3fn if fmt == MX_FP8 else torch.uint8)
+                or s.dtype is not torch.float8_e8m0fnu or c.shape[0] != rows or s.shape[0] != rows):
+            raise ValueError("codes (float8_e4m3fn for fp8, uint8 for fp4) and padded_scales (float8_e8m0fnu) must be 2-D "
+                             "with unit column stride, on one device, a row for each row (tiled: each 32)")
+        # one row has whatever stride: its leading dimension is its length
+        self._set(c, s, R, K, fmt, layout, dev, c.stride(0) if rows > 1 else c.shape[1],
+                  s.stride(0) if rows > 1 else s.shape[1])
+
+    def _set(self, c, s, R, K, fmt, layout, dev, ld_c, ld_s):
+        self._codes, self._scales, self._R, self._K, self._fmt, self._layout, self._device = c, s, R, K, fmt, layout, dev
+        self._c = _abi.Mx(c.data_ptr(), ld_c, s.data_ptr(), ld_s, R, K, fmt, layout)
+        self._ref = ctypes.byref(self._c)
+
+    codes = property(lambda self: self._codes)
+    padded_scales = property(lambda self: self._scales)
+    R = property(lambda self: self._R)
+    K = property(lambda self: self._K)
+    fmt = property(lambda self: self._fmt)
+    layout = property(lambda self: self._layout)
+    device = property(lambda self: self._device)
 
     @classmethod
     def empty(cls, R: int, K: int, fmt: int, device, layout: int = MX_ROWS) -> "MxTensor":
         """Storage for mx_quantize, rmsnorm or mx_pack to write."""
         torch = _torch()
-        if fmt not in (MX_FP4, MX_FP8):
+        steps, chunks = -(-K // _STEP), -(-K // _CHUNK)
+        if fmt == MX_FP8:
+            t, c = torch.float8_e4m3fn, steps * 128
+        elif fmt == MX_FP4:
+            t, c = torch.uint8, steps * 64
+        else:
             raise ValueError(f"unknown format {fmt}")
-        steps, chunks = _up(K, _STEP), _up(K, _CHUNK)
+        rows, s = R, chunks * 16
         if layout == MX_TILED:
             rows, c, s = _up(R, _TILE), steps * 2048, chunks * 512
-        else:
-            rows, c, s = R, steps * (64 if fmt == MX_FP4 else 128), chunks * 16
-        t = torch.float8_e4m3fn if fmt == MX_FP8 else torch.uint8
-        return cls(torch.empty((rows, c), dtype=t, device=device),
-                   torch.empty((rows, s), dtype=torch.uint8, device=device), R, K, fmt, layout)
+        q = cls.__new__(cls)
+        codes = torch.empty((rows, c), dtype=t, device=device)
+        q._set(codes, torch.empty((rows, s), dtype=torch.float8_e8m0fnu, device=device), R, K, fmt, layout, codes.device,
+               c, s)
+        return q
 
     @classmethod
     def from_tensors(cls, codes, scales, K: int, fmt: int) -> "MxTensor":
@@ -103,98 +127,95 @@ class MxTensor:
             raise ValueError(f"K={K} (a multiple of 8) takes codes [R][{blocks * per}] and scales [R][{blocks}], got "
                              f"{list(codes.shape)} and {list(scales.shape)}")
         q = cls.empty(R, K, fmt, codes.device)
-        c = q.codes.view(torch.uint8)
+        c, s = q.codes.view(torch.uint8), q.padded_scales.view(torch.uint8)
         used = K // 2 if fmt == MX_FP4 else K
         c[:, :used] = codes.view(torch.uint8)[:, :used]
         c[:, used:] = 0
-        q.scale_bytes[:, :blocks] = scales.view(torch.uint8)
-        q.scale_bytes[:, blocks:] = 0
+        s[:, :blocks] = scales.view(torch.uint8)
+        s[:, blocks:] = 0
         return q
-
-    @property
-    def device(self):
-        return self.codes.device
 
     @property
     def scales(self):
         """MX_ROWS: the scales' values, float8_e8m0fnu [R][ceil(K/32)]."""
-        torch = _torch()
-        if self.layout != MX_ROWS:
+        if self._layout != MX_ROWS:
             raise ValueError("a tiled tensor has no scales by rows")
-        return self.scale_bytes[:, :_up(self.K, _BLOCK)].view(torch.float8_e8m0fnu)
-
-    def c_struct(self) -> _abi.Mx:
-        torch = _torch()
-        c, s = self.codes, self.scale_bytes
-        if (c.dim() != 2 or s.dim() != 2 or c.stride(1) != 1 or s.stride(1) != 1 or c.device != s.device
-                or c.dtype is not (torch.float8_e4m3fn if self.fmt == MX_FP8 else torch.uint8)
-                or s.dtype is not torch.uint8 or c.shape[0] != s.shape[0]
-                or c.shape[0] != (self.R if self.layout == MX_ROWS else _up(self.R, _TILE))):
-            raise ValueError("codes and scale_bytes must be 2-D with unit column stride, on one device, a row for each "
-                             "row (tiled: each 32), of float8_e4m3fn (fp8) or uint8 (fp4) and of uint8")
-        _gpu(c, "an MX tensor")
-        # rows further apart than their number of rows asks for: one row has any stride
-        ld_c = c.stride(0) if c.shape[0] > 1 else c.shape[1]
-        ld_s = s.stride(0) if s.shape[0] > 1 else s.shape[1]
-        return _abi.Mx(c.data_ptr(), ld_c, s.data_ptr(), ld_s, self.R, self.K, self.fmt, self.layout)
+        n = -(-self._K // _BLOCK)
+        return self._scales if self._scales.shape[1] == n else self._scales[:, :n]
 
     def column_shard(self, rank: int, tp: int) -> "MxTensor":
         """Column-parallel share of a weight (views): outputs [rank*R/tp, ...)."""
-        n = self.R // tp
+        n = self._R // tp
         r0 = rank * n
-        if self.layout == MX_TILED:
+        if self._layout == MX_TILED:
             if n % _TILE and tp > 1:
                 raise ValueError("a tiled column shard must start and end on 32-row tiles")
             a, b = r0 // _TILE, _up(r0 + n, _TILE)
         else:
             a, b = r0, r0 + n
-        return MxTensor(self.codes[a:b], self.scale_bytes[a:b], n, self.K, self.fmt, self.layout)
+        return MxTensor(self._codes[a:b], self._scales[a:b], n, self._K, self._fmt, self._layout)
 
     def row_shard(self, rank: int, tp: int) -> "MxTensor":
         """Row-parallel share of a weight (views): inputs [rank*K/tp, ...)."""
-        k = self.K // tp
+        k = self._K // tp
         if k % _CHUNK and tp > 1:
             raise ValueError("a row shard must start and end on multiples of 512 inputs")
         if tp == 1:
             return self
         steps, chunks = k // _STEP, k // _CHUNK
-        per_c, per_s = (2048, 512) if self.layout == MX_TILED else (64 if self.fmt == MX_FP4 else 128, 16)
-        return MxTensor(self.codes[:, rank * steps * per_c:(rank + 1) * steps * per_c],
-                        self.scale_bytes[:, rank * chunks * per_s:(rank + 1) * chunks * per_s],
-                        self.R, k, self.fmt, self.layout)
+        per_c, per_s = (2048, 512) if self._layout == MX_TILED else (64 if self._fmt == MX_FP4 else 128, 16)
+        return MxTensor(self._codes[:, rank * steps * per_c:(rank + 1) * steps * per_c],
+                        self._scales[:, rank * chunks * per_s:(rank + 1) * chunks * per_s],
+                        self._R, k, self._fmt, self._layout)
+
+
+def _mx_arg(name, q, device=None, layout=None):
+    if not isinstance(q, MxTensor):
+        raise TypeError(f"{name} must be an MxTensor, got {type(q).__name__}")
+    if q._device.type != "cuda":
+        raise ValueError(f"{name} must be on a GPU, got {q._device}")
+    if device is not None and q._device != device:
+        raise ValueError(f"{name} is on {q._device}, X on {device}")
+    return q._ref
+
+
+def _mx_out(out, M, K, fmt, device):
+    if out is None:
+        return MxTensor.empty(M, K, fmt, device)
+    _mx_arg("out", out, device)
+    if (out._R, out._K, out._fmt, out._layout) != (M, K, fmt, MX_ROWS):
+        raise ValueError("out must be an MxTensor of X's shape, the format asked for and the MX_ROWS layout")
+    return out
 
 
 def mx_quantize(X, fmt: int, out: Optional[MxTensor] = None) -> MxTensor:
     """X [R][K] (fp16 or bf16, K a multiple of 8) in MX numbers of format fmt."""
     _rows16("X", X)
-    _gpu(X, "X")
-    if out is None:
-        out = MxTensor.empty(X.shape[0], X.shape[1], fmt, X.device)
-    elif (out.R, out.K, out.fmt, out.layout) != (X.shape[0], X.shape[1], fmt, MX_ROWS):
-        raise ValueError("out must have X's shape, the format asked for and the MX_ROWS layout")
-    _same_device(X.device, out=out)
-    cq = out.c_struct()
-    _run(X.device, _abi.lib().tpdq_mx_quantize, X.data_ptr(), X.stride(0), _dtype_code(X.dtype), ctypes.byref(cq))
+    dev = _device_of("X", X)
+    out = _mx_out(out, X.shape[0], X.shape[1], fmt, dev)
+    _run(dev, _abi.lib().tpdq_mx_quantize, X.data_ptr(), X.stride(0), _dtype_code(X.dtype), out._ref)
     return out
 
 
 def mx_dequantize(q: MxTensor, dtype, out=None):
     """The values of an MX_ROWS tensor, rounded once to fp16 or bf16."""
-    torch = _torch()
+    ref = _mx_arg("q", q)
+    dev = q._device
+    code = _dtype_code(dtype)
     if out is None:
-        out = torch.empty((q.R, q.K), dtype=dtype, device=q.device)
-    _rows16("out", out, (q.R, q.K), dtype)
-    _same_device(q.device, out=out)
-    cq = q.c_struct()
-    _run(q.device, _abi.lib().tpdq_mx_dequantize, ctypes.byref(cq), _dtype_code(dtype), out.data_ptr(), out.stride(0))
+        out = _torch().empty((q._R, q._K), dtype=dtype, device=dev)
+    else:
+        _rows16("out", out, q._R, q._K, dtype)
+        _same_device(dev, "out", out)
+    _run(dev, _abi.lib().tpdq_mx_dequantize, ref, code, out.data_ptr(), out.stride(0))
     return out
 
 
 def mx_pack(q: MxTensor) -> MxTensor:
     """An fp4 weight [N][K] in the order that the products read (offline)."""
-    out = MxTensor.empty(q.R, q.K, q.fmt, q.device, MX_TILED)
-    a, b = q.c_struct(), out.c_struct()
-    _run(q.device, _abi.lib().tpdq_mx_pack, ctypes.byref(a), ctypes.byref(b))
+    ref = _mx_arg("q", q)
+    out = MxTensor.empty(q._R, q._K, q._fmt, q._device, MX_TILED)
+    _run(q._device, _abi.lib().tpdq_mx_pack, ref, out._ref)
     return out
 
 
@@ -204,61 +225,78 @@ def rmsnorm(X, weight, eps: float, residual=None, fmt: Optional[int] = None, res
     as an MxTensor; h in residual_out (which may be residual itself) or new."""
     torch = _torch()
     _rows16("X", X)
-    _gpu(X, "X")
+    dev, dt = _device_of("X", X), X.dtype
     M, K = X.shape
-    dev = X.device
+    code = _dtype_code(dt)
     if weight.dim() != 1 or weight.shape[0] != K or not weight.is_contiguous():
         raise ValueError(f"weight must be a contiguous [{K}]")
-    if weight.dtype != X.dtype:
-        raise TypeError(f"weight is {weight.dtype}, X is {X.dtype}: one element type per call")
-    h, ldr, ldh = X, 0, 0
+    if weight.dtype != dt:
+        raise TypeError(f"weight is {weight.dtype}, X is {dt}: one element type per call")
+    _same_device(dev, "weight", weight)
+    h, res, ldr, hp, ldh = X, None, 0, None, 0
     if residual is not None:
-        _rows16("residual", residual, (M, K), X.dtype)
-        h = torch.empty((M, K), dtype=X.dtype, device=dev) if residual_out is None else residual_out
-        _rows16("residual_out", h, (M, K), X.dtype)
-        ldr, ldh = residual.stride(0), h.stride(0)
+        _rows16("residual", residual, M, K, dt)
+        _same_device(dev, "residual", residual)
+        if residual_out is None:
+            h = torch.empty((M, K), dtype=dt, device=dev)
+        else:
+            h = residual_out
+            _rows16("residual_out", h, M, K, dt)
+            _same_device(dev, "residual_out", h)
+        res, ldr, hp, ldh = residual.data_ptr(), residual.stride(0), h.data_ptr(), h.stride(0)
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
-    y = cq = None
     if fmt is None:
-        y = torch.empty((M, K), dtype=X.dtype, device=dev) if out is None else out
-        _rows16("out", y, (M, K), X.dtype)
+        if out is None:
+            out = torch.empty((M, K), dtype=dt, device=dev)
+        else:
+            _rows16("out", out, M, K, dt)
+            _same_device(dev, "out", out)
+        y, ldy, ref = out.data_ptr(), out.stride(0), None
     else:
-        out = MxTensor.empty(M, K, fmt, dev) if out is None else out
-        if not isinstance(out, MxTensor) or (out.R, out.K, out.fmt, out.layout) != (M, K, fmt, MX_ROWS):
-            raise ValueError("out must be an MxTensor of X's shape, the format asked for and the MX_ROWS layout")
-        cq = out.c_struct()
-    _same_device(dev, weight=weight, residual=residual, residual_out=h, out=out if y is None else y)
-    _run(dev, _abi.lib().tpdq_rmsnorm, X.data_ptr(), X.stride(0), None if residual is None else residual.data_ptr(), ldr,
-         weight.data_ptr(), eps, M, K, _dtype_code(X.dtype), None if residual is None else h.data_ptr(), ldh,
-         None if y is None else y.data_ptr(), 0 if y is None else y.stride(0), None if cq is None else ctypes.byref(cq))
-    return (out if y is None else y), h
+        out = _mx_out(out, M, K, fmt, dev)
+        y, ldy, ref = None, 0, out._ref
+    _run(dev, _abi.lib().tpdq_rmsnorm, X.data_ptr(), X.stride(0), res, ldr, weight.data_ptr(), eps, M, K, code, hp, ldh,
+         y, ldy, ref)
+    return out, h
+
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(op: int, M: int, R: int, K: int, R2: int) -> int:
+    """tpdq_mx_workspace_bytes: of the sizes alone."""
+    a = _abi.Mx(None, 0, None, 0, R, K, MX_FP4, MX_TILED)
+    b = _abi.Mx(None, 0, None, 0, R2, R, MX_FP4, MX_TILED)
+    return _abi.lib().tpdq_mx_workspace_bytes(op, M, ctypes.byref(a), ctypes.byref(b) if R2 else None)
 
 
 def _scratch(workspace: Optional[Workspace], nbytes: int, device):
-    """The caller's workspace, or one of the call's own: calls that are captured
-    in two graphs, or run on two streams, share none."""
-    torch = _torch()
-    if workspace is not None:
-        return workspace.get(nbytes)
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    """(address, bytes) and the tensor that holds it: the caller's workspace, or one
+    of the call's own, so that calls captured in two graphs, or running on two
+    streams, share none."""
+    if not nbytes:
+        return None, 0, None
+    buf = workspace.get(nbytes) if workspace is not None else _torch().empty(nbytes, dtype=_torch().uint8, device=device)
+    return buf.data_ptr(), buf.numel(), buf
+
+
+def _out16(out, M, N, dtype, device):
+    if out is None:
+        return _torch().empty((M, N), dtype=dtype, device=device)
+    _rows16("out", out, M, N, dtype)
+    _same_device(device, "out", out)
+    return out
 
 
 def mx_gemm(X: MxTensor, w: MxTensor, dtype, out=None, workspace: Optional[Workspace] = None):
     """Y = X W^T: X [M][K] fp8 or fp4, w [N][K] fp4 from mx_pack, fp32 accumulation,
     Y [M][N] rounded once to dtype."""
-    torch = _torch()
-    dev = X.device
-    _same_device(dev, w=w, out=out)
-    if out is None:
-        out = torch.empty((X.R, w.R), dtype=dtype, device=dev)
-    _rows16("out", out, (X.R, w.R), dtype)
-    cx, cw = X.c_struct(), w.c_struct()
-    lib = _abi.lib()
-    nbytes = lib.tpdq_mx_workspace_bytes(_abi.OP_MX_GEMM, X.R, ctypes.byref(cw), None)
-    buf = _scratch(workspace, nbytes, dev)
-    _run(dev, lib.tpdq_mx_gemm, ctypes.byref(cx), ctypes.byref(cw), _dtype_code(dtype), out.data_ptr(), out.stride(0),
-         None if buf is None else buf.data_ptr(), 0 if buf is None else buf.numel())
+    cx = _mx_arg("X", X)
+    dev = X._device
+    cw = _mx_arg("w", w, dev)
+    code = _dtype_code(dtype)
+    out = _out16(out, X._R, w._R, dtype, dev)
+    ws, nbytes, _buf = _scratch(workspace, _workspace_bytes(_abi.OP_MX_GEMM, X._R, w._R, w._K, 0), dev)
+    _run(dev, _abi.lib().tpdq_mx_gemm, cx, cw, code, out.data_ptr(), out.stride(0), ws, nbytes)
     return out
 
 
@@ -267,20 +305,16 @@ def mx_mlp_shard(X: MxTensor, w_up: MxTensor, w_down: MxTensor, dtype, w_gate: O
     """One rank's MLP share up to the AllReduce: Y1 = X W_up^T, or silu(X W_gate^T)
     * (X W_up^T) with w_gate, quantized in X's format; returns Y2_partial = Y1
     W_down^T. w_up and w_gate are column shards, w_down a row shard."""
-    torch = _torch()
-    dev = X.device
-    _same_device(dev, w_up=w_up, w_down=w_down, w_gate=w_gate, out=out)
-    if out is None:
-        out = torch.empty((X.R, w_down.R), dtype=dtype, device=dev)
-    _rows16("out", out, (X.R, w_down.R), dtype)
-    if X.R > 1 and out.stride(0) != w_down.R:
+    cx = _mx_arg("X", X)
+    dev = X._device
+    cu, cd = _mx_arg("w_up", w_up, dev), _mx_arg("w_down", w_down, dev)
+    cg = None if w_gate is None else _mx_arg("w_gate", w_gate, dev)
+    code = _dtype_code(dtype)
+    if w_down._K != w_up._R:
+        raise ValueError(f"w_down takes {w_down._K} inputs, w_up has {w_up._R} outputs")
+    out = _out16(out, X._R, w_down._R, dtype, dev)
+    if X._R > 1 and out.stride(0) != w_down._R:
         raise ValueError("out must be dense")
-    cx, cu, cd = X.c_struct(), w_up.c_struct(), w_down.c_struct()
-    cg = None if w_gate is None else w_gate.c_struct()
-    lib = _abi.lib()
-    nbytes = lib.tpdq_mx_workspace_bytes(_abi.OP_MX_MLP, X.R, ctypes.byref(cu), ctypes.byref(cd))
-    buf = _scratch(workspace, nbytes, dev)
-    _run(dev, lib.tpdq_mx_mlp_shard, ctypes.byref(cx), None if cg is None else ctypes.byref(cg), ctypes.byref(cu),
-         ctypes.byref(cd), _dtype_code(dtype), out.data_ptr(), None if buf is None else buf.data_ptr(),
-         0 if buf is None else buf.numel())
+    ws, nbytes, _buf = _scratch(workspace, _workspace_bytes(_abi.OP_MX_MLP, X._R, w_up._R, w_up._K, w_down._R), dev)
+    _run(dev, _abi.lib().tpdq_mx_mlp_shard, cx, cg, cu, cd, code, out.data_ptr(), ws, nbytes)
     return out

@@ -65,7 +65,7 @@ def quantized(M, K, fmt, seed, dev):
 def raw(q):
     """(codes one each, scale bytes, all code bytes, all scale bytes) of an MX_ROWS tensor"""
     import torch
-    c, s = q.codes.view(torch.uint8).cpu().numpy(), q.scale_bytes.cpu().numpy()
+    c, s = q.codes.view(torch.uint8).cpu().numpy(), q.padded_scales.view(torch.uint8).cpu().numpy()
     return ref.unpack_bytes(c, q.K, q.fmt), s[:, :-(-q.K // 32)], c, s
 
 
@@ -168,7 +168,7 @@ def test_pack(N, K):
     w = tpdq.mx_pack(q)
     c, s = ref.tiled(codes, sb)
     np.testing.assert_array_equal(w.codes.cpu().numpy(), c)
-    np.testing.assert_array_equal(w.scale_bytes.cpu().numpy(), s)
+    np.testing.assert_array_equal(w.padded_scales.view(torch.uint8).cpu().numpy(), s)
 
 
 def test_past_32_bits():
@@ -181,7 +181,7 @@ def test_past_32_bits():
     q = tpdq.mx_quantize(x, tpdq.MX_FP8)
     tail = tpdq.mx_quantize(x[-3:], tpdq.MX_FP8)
     assert torch.equal(q.codes[-3:].view(torch.uint8), tail.codes.view(torch.uint8))
-    assert torch.equal(q.scale_bytes[-3:], tail.scale_bytes)
+    assert torch.equal(q.padded_scales[-3:].view(torch.uint8), tail.padded_scales.view(torch.uint8))
     w = torch.ones(K, dtype=torch.bfloat16, device=dev)
     y, _ = tpdq.rmsnorm(x, w, 1e-5, out=x)  # a row is read before it is written
     want, _ = tpdq.rmsnorm(acts(3, K, 5, dev, "bf16"), w, 1e-5)
@@ -355,10 +355,10 @@ def test_product_not_finite(fmt, M):
     dev = u.torch_dev()
     N, K = 96, 1096
     q, x = quantized(M, K, fmt, 4, dev)
-    q.scale_bytes[M // 2, 3] = 255
+    q.padded_scales.view(torch.uint8)[M // 2, 3] = 255
     w0, wv = weight(N, K, 5, dev)
-    w = tpdq.MxTensor(w0.codes.clone(), w0.scale_bytes.clone(), N, K, w0.fmt, w0.layout)
-    w.scale_bytes[1, 512 + 8 * 5 + 1] = 255  # tile 1, chunk 1, lane 5, operand 0, step 1: row 32 + 8 + 1
+    w = tpdq.MxTensor(w0.codes.clone(), w0.padded_scales.clone(), N, K, w0.fmt, w0.layout)
+    w.padded_scales.view(torch.uint8)[1, 512 + 8 * 5 + 1] = 255  # tile 1, chunk 1, lane 5, operand 0, step 1: row 32 + 8 + 1
     y = f64(tpdq.mx_gemm(q, w, torch.bfloat16))
     bad = np.zeros((M, N), bool)
     bad[M // 2], bad[:, 41] = True, True
@@ -573,4 +573,11 @@ def test_binding_refuses():
     with pytest.raises(tpdq.TpdqError):
         tpdq.rmsnorm(x, nw, -1.0)
     with pytest.raises(ValueError):
-        tpdq.mx_mlp_shard(q, w, w, torch.float16, out=torch.empty(4, 128, dtype=torch.float16, device=dev)[:, :64])
+        tpdq.mx_mlp_shard(q, w, w, torch.float16)                       # 64 outputs, 256 inputs
+    with pytest.raises(TypeError):
+        tpdq.mx_gemm(x, w, torch.float16)
+    with pytest.raises(AttributeError):
+        w.codes = w.codes
+    d, _ = weight(64, 64, 3, dev)
+    with pytest.raises(ValueError):
+        tpdq.mx_mlp_shard(q, w, d, torch.float16, out=torch.empty(4, 128, dtype=torch.float16, device=dev)[:, :64])

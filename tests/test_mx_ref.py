@@ -200,6 +200,6 @@ def test_binding_refuses_on_the_host():
         w.row_shard(0, 2)                                     # 768 inputs: no whole chunks
     with pytest.raises(ValueError):
         w.scales
-    assert w.row_shard(1, 3).codes.shape == (3, 4 * 2048) and w.row_shard(1, 3).scale_bytes.shape == (3, 512)
+    assert w.row_shard(1, 3).codes.shape == (3, 4 * 2048) and w.row_shard(1, 3).padded_scales.shape == (3, 512)
     with pytest.raises(ValueError):
         tpdq.mx_gemm(tpdq.MxTensor.empty(1, 1536, tpdq.MX_FP8, "cpu"), w, torch.float16)
