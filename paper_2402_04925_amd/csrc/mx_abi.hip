@@ -55,10 +55,12 @@ tpdq_status check_rows16(const void* p, int64_t ld, int64_t K, const char* name)
 
 MxRows rows_of(const tpdq_mx* q) { return MxRows{(uint8_t*)q->codes, q->ld_c, (uint8_t*)q->scales, q->ld_s}; }
 
-// one thread per octet of a padded row, in workgroups of 256
+// A launch has fewer than 2^32 threads; the row-wise kernels and mx_pack take one
+// for 32 elements of rows padded to whole chunks (large calls).
 tpdq_status check_grid(int64_t R, int64_t K) {
-  if (R * mx_chunks(K) >= (int64_t)1 << 32)
-    return fail(TPDQ_ERR_UNSUPPORTED, "more than 2^31 workgroups: quantize rows in several calls");
+  if (R * mx_chunks(K) >= (int64_t)1 << 28)
+    return fail(TPDQ_ERR_UNSUPPORTED, "%lld rows of %lld: more threads than a launch has, split the rows", (long long)R,
+                (long long)K);
   return TPDQ_OK;
 }
 
@@ -178,6 +180,9 @@ tpdq_status tpdq_rmsnorm(const void* X, int64_t ldx, const void* residual, int64
       st = fail(TPDQ_ERR_SHAPE, "q is %d x %d, the call %d x %d", q->R, q->K, M, K);
   }
   if (st != TPDQ_OK) return st;
+  int vpt = 0;
+  if ((int64_t)M * norm_threads(K, q ? q->format : -1, &vpt) >= (int64_t)1 << 32)
+    return fail(TPDQ_ERR_UNSUPPORTED, "%d rows: more threads than a launch has, split the rows", M);
   NormArgs a{};
   a.X = (const uint16_t*)X;
   a.ldx = ldx;

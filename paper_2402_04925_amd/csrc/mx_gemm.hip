@@ -177,10 +177,9 @@ hipError_t rows_launch(const MxArgs& a, hipStream_t s) {
   constexpr int wave_lds = x > red ? x : red;
   static_assert((size_t)NWMAX * wave_lds <= kLdsMax, "");
   auto* k = k_mx_rows<DT, FMT, MT, TN, GATED, QUANT, NWMAX>;
-  if (NWMAX * wave_lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, NWMAX * wave_lds);
-    if (e != hipSuccess) return e;
-  }
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_lds((const void*)k, NWMAX * wave_lds, &done);
+  if (e != hipSuccess) return e;
   k<<<dim3((unsigned)(TN == 2 ? tiles : 2 * tiles)), dim3((unsigned)nw * 64), nw * wave_lds, s>>>(a);
   return hipGetLastError();
 }
@@ -285,6 +284,18 @@ MxPlan plan_mx(int M, int N, int K, int fmt, bool gated, bool quant) {
 
 size_t mx_part_bytes(const MxPlan& p, int M, int N, bool gated) {
   return p.ks > 1 ? align_up((size_t)p.ks * M * N * (gated ? 8 : 4)) : 0;
+}
+
+hipError_t allow_lds(const void* f, int bytes, std::atomic<uint64_t>* done) {
+  if (bytes <= 64 * 1024) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = (uint64_t)1 << (dev & 63);
+  if (dev < 64 && (done->load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess && dev < 64) done->fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 hipError_t launch_mx_gemm(MxArgs a, int dt, int fmt, float* part, hipStream_t s) {

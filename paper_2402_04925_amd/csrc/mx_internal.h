@@ -3,6 +3,8 @@
 // and the product's kernels.
 #pragma once
 
+#include <atomic>
+
 #include "tpdq_internal.h"
 
 namespace tpdq {
@@ -27,6 +29,11 @@ inline int64_t mx_row_scales(int64_t K) { return mx_chunks(K) * 16; }
 inline int64_t mx_tile_codes(int64_t K) { return mx_steps(K) * 2048; }
 inline int64_t mx_tile_scales(int64_t K) { return mx_chunks(K) * 512; }
 
+// Lets kernel f use `bytes` of LDS where that is more than the default: once for a
+// kernel (each has its own `done`) and device. A launch of a few microseconds would
+// feel it on every call.
+hipError_t allow_lds(const void* f, int bytes, std::atomic<uint64_t>* done);
+
 struct MxRows {  // a TPDQ_MX_ROWS tensor
   uint8_t* codes;
   int64_t ld_c;
@@ -43,6 +50,13 @@ hipError_t launch_mx_pack(const MxRows& q, int R, int K, uint8_t* codes, int64_t
 
 // Columns of a row that k_rmsnorm holds in a workgroup's registers
 constexpr int kNormMaxK = 65536;
+// Threads of a row's workgroup: one octet each as far as 1024 reach, then up to eight
+inline int norm_threads(int K, int fmt, int* octets_per_thread) {
+  const int octets = fmt < 0 ? K / 8 : (int)(mx_chunks(K) * 64);
+  const int waves = octets > 15 * 64 ? 16 : (octets + 63) / 64;
+  *octets_per_thread = (octets + 64 * waves - 1) / (64 * waves);
+  return 64 * waves;
+}
 struct NormArgs {
   const uint16_t* X;
   int64_t ldx;

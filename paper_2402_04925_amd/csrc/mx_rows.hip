@@ -13,55 +13,84 @@ namespace {
 
 constexpr int kRowThreads = 256;
 
-// One octet of a row per thread; a block's four lanes share their maximum. Rows
-// are padded to whole chunks of 512, so that the block's lanes are in one wave and
-// the padding's codes and scales are written (zeros).
-template <int DT, int FMT>
-__global__ __launch_bounds__(kRowThreads) void k_mx_quantize(const uint16_t* __restrict__ X, int64_t ldx,
-                                                             int64_t octets, int per_row, int K, MxRows q) {
-  const int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-  if (i >= octets) return;  // whole waves: octets is a multiple of 64
-  const int64_t r = i / per_row;
-  const int k8 = (int)(i - r * per_row);
-  u4_t x = {0u, 0u, 0u, 0u};
-  if (8 * k8 < K) x = *(const u4_t*)(X + r * ldx + 8 * k8);
-  float v[8];
-  unpack8<DT>(x, v);
-  store_mx8<FMT>(v, k8, 16 * ((K + kMxStep - 1) / kMxStep), q.codes + r * q.ld_c, q.scales + r * q.ld_s);
+// A workgroup takes up to 256 octets of ROWS consecutive rows, an octet of each row
+// per thread, all loads issued before the first is used; a block's four lanes share
+// their maximum. Rows are padded to whole chunks of 512, so that a block's lanes are
+// in one wave and the padding's codes and scales are written (zeros). seg: the
+// row's workgroups.
+template <int DT, int FMT, int ROWS>
+__global__ __launch_bounds__(kRowThreads) void k_mx_quantize(const uint16_t* __restrict__ X, int64_t ldx, int R, int seg,
+                                                             int per_row, int K, MxRows q) {
+  const int rb = blockIdx.x / seg;
+  const int k8 = (blockIdx.x - rb * seg) * blockDim.x + threadIdx.x;
+  if (k8 >= per_row) return;  // whole waves
+  const int64_t r0 = (int64_t)rb * ROWS;
+  const int code_octets = 16 * ((K + kMxStep - 1) / kMxStep);
+  u4_t x[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    x[i] = u4_t{0u, 0u, 0u, 0u};
+    if (8 * k8 < K && r0 + i < R) x[i] = *(const u4_t*)(X + (r0 + i) * ldx + 8 * k8);
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    if (r0 + i >= R) break;
+    float v[8];
+    unpack8<DT>(x[i], v);
+    store_mx8<FMT>(v, k8, code_octets, q.codes + (r0 + i) * q.ld_c, q.scales + (r0 + i) * q.ld_s);
+  }
 }
 
-template <int DT, int FMT>
-__global__ __launch_bounds__(kRowThreads) void k_mx_dequantize(MxRows q, int64_t octets, int per_row,
-                                                               uint16_t* __restrict__ X, int64_t ldx) {
-  const int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-  if (i >= octets) return;
-  const int64_t r = i / per_row;
-  const int k8 = (int)(i - r * per_row);
-  const uint32_t byte = q.scales[r * q.ld_s + (k8 >> 2)];
+template <int FMT>
+__device__ __forceinline__ void values8(u2_t w, uint32_t byte, float (&v)[8]) {
   // 2^(byte - 127); the smallest is subnormal
   const float s = byte == 255u ? __builtin_nanf("") : byte ? as_f32(byte << 23) : as_f32(0x00400000u);
-  float v[8];
-  if constexpr (FMT == kFp4) {
-    const uint32_t w = *(const uint32_t*)(q.codes + r * q.ld_c + 4 * k8);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t c = (w >> (4 * e)) & 0xFu, m = c & 7u;
+  for (int e = 0; e < 8; ++e) {
+    float a;
+    bool neg;
+    if constexpr (FMT == kFp4) {
+      const uint32_t c = (w.x >> (4 * e)) & 0xFu, m = c & 7u;
       // 0, 0.5, then (1 or 1.5) 2^(m / 2 - 1)
-      const float a = m < 2u ? 0.5f * (float)m : as_f32(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
-      v[e] = (c & 8u ? -a : a) * s;
-    }
-  } else {
-    const u2_t w = *(const u2_t*)(q.codes + r * q.ld_c + 8 * k8);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
+      a = m < 2u ? 0.5f * (float)m : as_f32(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
+      neg = c & 8u;
+    } else {
       const uint32_t c = (w[e >> 2] >> (8 * (e & 3))) & 0xFFu, m = c & 0x7Fu;
       // subnormal: m 2^-9; normal: the exponent's bias 7 against 127; NaN: 0x7F
-      float a = m < 8u ? (float)m * 0x1p-9f : as_f32((m << 20) + (120u << 23));
+      a = m < 8u ? (float)m * 0x1p-9f : as_f32((m << 20) + (120u << 23));
       if (m == 0x7Fu) a = __builtin_nanf("");
-      v[e] = (c & 0x80u ? -a : a) * s;
+      neg = c & 0x80u;
+    }
+    v[e] = (neg ? -a : a) * s;
+  }
+}
+
+template <int DT, int FMT, int ROWS>
+__global__ __launch_bounds__(kRowThreads) void k_mx_dequantize(MxRows q, int R, int seg, int per_row,
+                                                               uint16_t* __restrict__ X, int64_t ldx) {
+  const int rb = blockIdx.x / seg;
+  const int k8 = (blockIdx.x - rb * seg) * blockDim.x + threadIdx.x;
+  if (k8 >= per_row) return;
+  const int64_t r0 = (int64_t)rb * ROWS;
+  u2_t w[ROWS];
+  uint32_t byte[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    w[i] = u2_t{0u, 0u};
+    byte[i] = 0u;
+    if (r0 + i < R) {
+      byte[i] = q.scales[(r0 + i) * q.ld_s + (k8 >> 2)];
+      if constexpr (FMT == kFp4) w[i].x = *(const uint32_t*)(q.codes + (r0 + i) * q.ld_c + 4 * (int64_t)k8);
+      else w[i] = *(const u2_t*)(q.codes + (r0 + i) * q.ld_c + 8 * (int64_t)k8);
     }
   }
-  *(u4_t*)(X + r * ldx + 8 * k8) = pack8<DT>(v);
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    if (r0 + i >= R) break;
+    float v[8];
+    values8<FMT>(w[i], byte[i], v);
+    *(u4_t*)(X + (r0 + i) * ldx + 8 * (int64_t)k8) = pack8<DT>(v);
+  }
 }
 
 // Rows -> 32-row tiles. A thread moves one lane's 16 bytes: tile T, step s,
@@ -187,28 +216,50 @@ unsigned blocks_of(int64_t n) { return (unsigned)((n + kRowThreads - 1) / kRowTh
 
 }  // namespace
 
+namespace {
+
+// Rows of a workgroup: four where that leaves every CU its eight workgroups
+template <typename F1, typename F4>
+hipError_t by_rows(int R, int per_row, F1 one, F4 four) {
+  const int seg = (per_row + kRowThreads - 1) / kRowThreads;
+  const int threads = std::min(kRowThreads, ((per_row + seg - 1) / seg + 63) / 64 * 64);
+  if ((int64_t)R * seg >= 4 * 2048) four(dim3((unsigned)(((int64_t)R + 3) / 4 * seg)), dim3((unsigned)threads), seg);
+  else one(dim3((unsigned)((int64_t)R * seg)), dim3((unsigned)threads), seg);
+  return hipGetLastError();
+}
+
+template <int DT, int FMT>
+hipError_t quantize(const uint16_t* X, int64_t ldx, int R, int K, const MxRows& q, hipStream_t s) {
+  const int per_row = (int)(mx_chunks(K) * 64);
+  return by_rows(
+      R, per_row,
+      [&](dim3 g, dim3 b, int seg) { k_mx_quantize<DT, FMT, 1><<<g, b, 0, s>>>(X, ldx, R, seg, per_row, K, q); },
+      [&](dim3 g, dim3 b, int seg) { k_mx_quantize<DT, FMT, 4><<<g, b, 0, s>>>(X, ldx, R, seg, per_row, K, q); });
+}
+
+template <int DT, int FMT>
+hipError_t dequantize(const MxRows& q, int R, int K, uint16_t* X, int64_t ldx, hipStream_t s) {
+  const int per_row = K / 8;
+  return by_rows(
+      R, per_row,
+      [&](dim3 g, dim3 b, int seg) { k_mx_dequantize<DT, FMT, 1><<<g, b, 0, s>>>(q, R, seg, per_row, X, ldx); },
+      [&](dim3 g, dim3 b, int seg) { k_mx_dequantize<DT, FMT, 4><<<g, b, 0, s>>>(q, R, seg, per_row, X, ldx); });
+}
+
+}  // namespace
+
 hipError_t launch_mx_quantize(const uint16_t* X, int64_t ldx, int R, int K, int dt, int fmt, const MxRows& q,
                               hipStream_t s) {
-  const int per_row = (int)(mx_chunks(K) * 64);
-  const int64_t n = (int64_t)R * per_row;
-  auto go = [&](auto* k) {
-    k<<<dim3(blocks_of(n)), dim3(kRowThreads), 0, s>>>(X, ldx, n, per_row, K, q);
-    return hipGetLastError();
-  };
-  if (dt == TPDQ_BF16) return fmt == kFp4 ? go(k_mx_quantize<kBF16, kFp4>) : go(k_mx_quantize<kBF16, kFp8>);
-  return fmt == kFp4 ? go(k_mx_quantize<kF16, kFp4>) : go(k_mx_quantize<kF16, kFp8>);
+  if (dt == TPDQ_BF16)
+    return fmt == kFp4 ? quantize<kBF16, kFp4>(X, ldx, R, K, q, s) : quantize<kBF16, kFp8>(X, ldx, R, K, q, s);
+  return fmt == kFp4 ? quantize<kF16, kFp4>(X, ldx, R, K, q, s) : quantize<kF16, kFp8>(X, ldx, R, K, q, s);
 }
 
 hipError_t launch_mx_dequantize(const MxRows& q, int R, int K, int dt, int fmt, uint16_t* X, int64_t ldx,
                                 hipStream_t s) {
-  const int per_row = K / 8;
-  const int64_t n = (int64_t)R * per_row;
-  auto go = [&](auto* k) {
-    k<<<dim3(blocks_of(n)), dim3(kRowThreads), 0, s>>>(q, n, per_row, X, ldx);
-    return hipGetLastError();
-  };
-  if (dt == TPDQ_BF16) return fmt == kFp4 ? go(k_mx_dequantize<kBF16, kFp4>) : go(k_mx_dequantize<kBF16, kFp8>);
-  return fmt == kFp4 ? go(k_mx_dequantize<kF16, kFp4>) : go(k_mx_dequantize<kF16, kFp8>);
+  if (dt == TPDQ_BF16)
+    return fmt == kFp4 ? dequantize<kBF16, kFp4>(q, R, K, X, ldx, s) : dequantize<kBF16, kFp8>(q, R, K, X, ldx, s);
+  return fmt == kFp4 ? dequantize<kF16, kFp4>(q, R, K, X, ldx, s) : dequantize<kF16, kFp8>(q, R, K, X, ldx, s);
 }
 
 hipError_t launch_mx_pack(const MxRows& q, int R, int K, uint8_t* codes, int64_t ld_c, uint8_t* scales,
@@ -225,17 +276,15 @@ hipError_t launch_mx_pack(const MxRows& q, int R, int K, uint8_t* codes, int64_t
   return hipGetLastError();
 }
 
-// Threads of a row: one octet each as far as 1024 threads reach, up to eight.
 hipError_t launch_rmsnorm(const NormArgs& a, int dt, int fmt, hipStream_t s) {
-  const int octets = fmt < 0 ? a.K / 8 : (int)(mx_chunks(a.K) * 64);
-  const int waves = std::min(16, (octets + 63) / 64);
-  const int vpt = (octets + 64 * waves - 1) / (64 * waves);
+  int vpt = 0;
+  const int threads = norm_threads(a.K, fmt, &vpt);
   if (dt == TPDQ_BF16) {
-    if (fmt < 0) return norm_launch<kBF16, -1>(a, 64 * waves, vpt, s);
-    return fmt == kFp4 ? norm_launch<kBF16, kFp4>(a, 64 * waves, vpt, s) : norm_launch<kBF16, kFp8>(a, 64 * waves, vpt, s);
+    if (fmt < 0) return norm_launch<kBF16, -1>(a, threads, vpt, s);
+    return fmt == kFp4 ? norm_launch<kBF16, kFp4>(a, threads, vpt, s) : norm_launch<kBF16, kFp8>(a, threads, vpt, s);
   }
-  if (fmt < 0) return norm_launch<kF16, -1>(a, 64 * waves, vpt, s);
-  return fmt == kFp4 ? norm_launch<kF16, kFp4>(a, 64 * waves, vpt, s) : norm_launch<kF16, kFp8>(a, 64 * waves, vpt, s);
+  if (fmt < 0) return norm_launch<kF16, -1>(a, threads, vpt, s);
+  return fmt == kFp4 ? norm_launch<kF16, kFp4>(a, threads, vpt, s) : norm_launch<kF16, kFp8>(a, threads, vpt, s);
 }
 
 }  // namespace tpdq

@@ -256,15 +256,14 @@ hipError_t tiles_launch(const MxArgs& a, hipStream_t s) {
   constexpr int BM = 16 * RT * WM;
   constexpr int lds = 2 * BM * (S * (FMT == kFp4 ? 64 : 128) + 16);
   auto* k = k_mx_tiles<DT, FMT, RT, WM, NP, NW, S, GATED, QUANT>;
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-  }
+  static std::atomic<uint64_t> done{0};
+  hipError_t e = allow_lds((const void*)k, lds, &done);
+  if (e != hipSuccess) return e;
   const int tiles = (int)(QUANT && a.ks == 1 ? mx_chunks(a.N) * (kMxChunk / kMxTile) : (a.N + kMxTile - 1) / kMxTile);
   const int per = (GATED ? 1 : NP) * NW / WM;
   const int64_t grid = (int64_t)((a.M + BM - 1) / BM) * ((tiles + per - 1) / per) * a.ks;
   k<<<dim3((unsigned)grid), dim3(NW * 64), lds, s>>>(a);
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess || a.ks == 1) return e;
   const int per_row = QUANT ? (int)(mx_chunks(a.N) * 64) : a.N / 8;
   const int64_t n = (int64_t)a.M * per_row;

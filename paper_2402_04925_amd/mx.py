@@ -24,11 +24,11 @@ def _up(a: int, b: int) -> int:
 
 def _run(device, f, *args):
     """f(*args, stream) with the tensors' device current (a launch needs that)."""
-    torch = _torch()
-    if device.index is None or device.index == torch.cuda.current_device():
+    cuda = _torch().cuda
+    if device.index is None or device.index == cuda.current_device():
         st = f(*args, _stream_handle(device))
     else:
-        with torch.cuda.device(device):
+        with cuda.device(device):
             st = f(*args, _stream_handle(device))
     if st:
         _abi.check(st)

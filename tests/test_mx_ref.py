@@ -129,6 +129,8 @@ def test_pack_refusals(lib):
     assert f(b=tiled(ld_c=2048)) == _abi.ERR_SHAPE and f(b=tiled(ld_s=256)) == _abi.ERR_SHAPE
     assert f(b=tiled(ld_s=520)) == _abi.ERR_ALIGN
     assert f(a=dst, b=dst) == _abi.ERR_SHAPE
+    huge = 1 << 28
+    assert f(a=rows(R=huge, fmt=_abi.MX_FP4), b=tiled(N=huge)) == _abi.ERR_UNSUPPORTED
 
 
 @needs_no_gpu
@@ -146,6 +148,8 @@ def test_rmsnorm_refusals(lib):
     assert f(ldx=260) == _abi.ERR_ALIGN and f(w=(1 << 31) + 8) == _abi.ERR_ALIGN and f(Y=(1 << 32) + 8) == _abi.ERR_ALIGN
     r = dict(res=1 << 33, h=1 << 34)
     assert f(**r, ldr=128) == _abi.ERR_SHAPE and f(**r, ldh=128) == _abi.ERR_SHAPE and f(**r, ldr=260) == _abi.ERR_ALIGN
+    big = dict(M=1 << 22, K=8192, ldx=8192, ldy=8192)
+    assert f(**big) == _abi.ERR_UNSUPPORTED                                       # 2^32 threads
     assert f(Y=None, q=rows(R=5)) == _abi.ERR_SHAPE and f(Y=None, q=rows(K=384)) == _abi.ERR_SHAPE
 
 
