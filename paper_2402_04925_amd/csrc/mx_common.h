@@ -134,9 +134,11 @@ __device__ __forceinline__ int xcd_run(int b, int nb) {
   return x * q + min(x, rem) + (b >> 3);
 }
 
-// 16 bytes per lane from global memory straight to LDS (dst + 16 lane)
+// BYTES per lane from global memory straight to LDS (dst + BYTES * lane)
+template <int BYTES>
 __device__ __forceinline__ void dma_lds(__amdgpu_buffer_rsrc_t r, void* dst, uint32_t off, uint32_t soff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 16, off, soff, 0, 0);
+  if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 16, off, soff, 0, 0);
+  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)dst, 4, off, soff, 0, 0);
 }
 
 // 8 outputs of a lane in 16 bits, or quantized into X's format (the block's four

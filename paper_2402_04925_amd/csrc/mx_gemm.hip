@@ -56,15 +56,15 @@ __global__ __launch_bounds__(NWMAX * 64) void k_mx_rows(MxArgs a) {
 #pragma unroll
   for (int t = 0; t < 2 * MT; ++t) {  // 8 rows each; lane: row lane / 8, chunk of 16 bytes swapped as in LDS
     const int m = 8 * t + (lane >> 3);
-    offx[t] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 16u * (uint32_t)((lane & 7) ^ (4 * (t & 1) + (lane >> 4)))
+    offx[t] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 16u * (uint32_t)((lane & 7) ^ (lane >> 3))
                       : kOutOfRange;
   }
 #pragma unroll
   for (int t = 0; t < MT; ++t) offxs[t] = 16 * t + r < a.M ? (uint32_t)(16 * t + r) * (uint32_t)a.x.ld_s : kOutOfRange;
   const uint32_t offw = T < tiles ? (uint32_t)T * (uint32_t)a.ldwc + 1024u * j0 + 16u * lane : kOutOfRange;
   const uint32_t offs = T < tiles ? (uint32_t)T * (uint32_t)a.ldws + 8u * lane : kOutOfRange;
-  // row r's chunk c of a line is at place c ^ (r / 2): the 16 rows in all 64 banks
-  const int xpos0 = r * 128 + ((g ^ (r >> 1)) << 4), xpos1 = xpos0 ^ 64;
+  // row r's chunk c of a line is at place c ^ (r % 8): 8 rows fill a 128-byte cycle
+  const int xpos0 = r * 128 + ((g ^ (r & 7)) << 4), xpos1 = xpos0 ^ 64;
 
   f4_t acc[MT][NT];
 #pragma unroll
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(NWMAX * 64) void k_mx_rows(MxArgs a) {
 #pragma unroll
       for (int t = 0; t < 2 * MT; ++t)
         if (8 * t < a.M)  // rows past M only reach outputs past M: their place may hold anything
-          dma_lds(rx, xl + ((t >> 1) * LINES + l) * 2048 + (t & 1) * 1024, offx[t],
+          dma_lds<16>(rx, xl + ((t >> 1) * LINES + l) * 2048 + (t & 1) * 1024, offx[t],
                   in ? (uint32_t)(c * LINES + l) * 128u : 0u);
     }
     __builtin_amdgcn_sched_barrier(0);

@@ -29,10 +29,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr int BM = 16 * RT * WM;
   static_assert(BM % 64 == 0 && (RT * WM * REC) % NW == 0 && (S == 2 || S == 4), "whole records, evenly over the waves");
   constexpr int XREC = RT * WM * REC / NW;     // ... per wave and block
-  constexpr int SREC = BM / 64;                // scale records (1 KB), one for each of the first waves
-  static_assert(SREC <= NW, "");
+  constexpr int SREC = BM / 16;                // scale records (256 B, a chunk's of 16 rows), one per wave
+  static_assert(SREC <= NW, "");               // (the same twice where there are more waves)
   constexpr int XBYTES = BM * REC * 64;
-  constexpr int STAGE = XBYTES + SREC * 1024;
+  constexpr int STAGE = XBYTES + SREC * 256;
   constexpr int ITEMS = XREC + 1;              // loads to LDS per wave and block
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 63;
@@ -68,12 +68,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     // record = (row tile, 128-byte line, half of the rows): 8 rows of one line
     const int rec = XREC * wave + k, rt = rec / REC, line = rec % REC / 2, hr = rec & 1;
     const int m = row0 + 16 * rt + 8 * hr + (lane >> 3);
-    const uint32_t chunk = (uint32_t)((lane & 7) ^ (4 * hr + (lane >> 4)));
+    const uint32_t chunk = (uint32_t)((lane & 7) ^ (lane >> 3));
     offx[k] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 128u * line + 16u * chunk : kOutOfRange;
   }
-  // a row's scales of the block's chunk, 16 bytes to a lane
-  const int ms = row0 + 64 * wave + lane;
-  const uint32_t offxs = wave < SREC && ms < a.M ? (uint32_t)ms * (uint32_t)a.x.ld_s : kOutOfRange;
+  // scale record in LDS: [word of the chunk][row], so that 16 rows' words are adjacent
+  const int ms = row0 + 16 * (wave % SREC) + r16;
+  const uint32_t offxs = ms < a.M ? (uint32_t)ms * (uint32_t)a.x.ld_s + 4u * g : kOutOfRange;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int T = GATED ? T0 : T0 + p;
@@ -81,38 +81,39 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     offws[p] = T < tiles ? (uint32_t)T * (uint32_t)a.ldws + 8u * lane : kOutOfRange;
   }
 
+  // All loads are unconditional and their conditions selects: a branch inside the
+  // block would let the compiler move the matrix instructions past it.
   auto dma_item = [&](int b, int st, int k) {
     unsigned char* sb = smem + st * STAGE;
     if (k < XREC) {
       const int line = (XREC * wave + k) % REC / 2;
-      const bool in = b < nblk && S * b + 2 * line / XW < steps;
+      const bool in = (b < nblk) & (S * b + 2 * line / XW < steps);
       const __amdgpu_buffer_rsrc_t r = buffer_rsrc(a.x.codes, in ? xbytes : 0u);
-      dma_lds(r, sb + (XREC * wave + k) * 1024, offx[k], in ? 64u * REC * (uint32_t)b : 0u);
-    } else if (wave < SREC) {
+      dma_lds<16>(r, sb + (XREC * wave + k) * 1024, offx[k], in ? 64u * REC * (uint32_t)b : 0u);
+    } else {
       const bool in = b < nblk;
       const __amdgpu_buffer_rsrc_t r = buffer_rsrc(a.x.scales, in ? xsbytes : 0u);
-      dma_lds(r, sb + XBYTES + wave * 1024, offxs, in ? (uint32_t)(S * b / 4) * 16u : 0u);
+      dma_lds<4>(r, sb + XBYTES + (wave % SREC) * 256, offxs, in ? ((uint32_t)(S * b) & ~3u) * 4u : 0u);
     }
   };
   auto load_w = [&](int b, int s, int i) {
-    const bool in = b < nblk && S * b + s < steps;
+    const bool in = (b < nblk) & (S * b + s < steps);
     const __amdgpu_buffer_rsrc_t r = buffer_rsrc(GATED && i >= 2 ? a.wc_up : a.wc, in ? wbytes : 0u);
     return __builtin_bit_cast(u4_t, __builtin_amdgcn_raw_buffer_load_b128(
         r, offw[i >> 1] + 1024u * (i & 1), in ? (uint32_t)(S * b + s) * 2048u : 0u, 0));
   };
-  // scale words of both operands of tile p: bytes of the chunk's steps, the block's
-  // steps lowest
+  // scale words of both operands of tile p: a byte for each step of the block's chunk
   auto load_ws = [&](int b, int p) {
     const bool in = b < nblk;
     const __amdgpu_buffer_rsrc_t r = buffer_rsrc(GATED && p ? a.ws_up : a.ws, in ? wsbytes : 0u);
     return __builtin_bit_cast(u2_t, __builtin_amdgcn_raw_buffer_load_b64(
-        r, offws[p], in ? (uint32_t)(S * b / 4) * 512u : 0u, 0));
+        r, offws[p], in ? ((uint32_t)(S * b) & ~3u) * 128u : 0u, 0));
   };
 
   // A 16-row tile's line in LDS: rows 128 bytes apart, the 16-byte chunk c of row r
-  // at place c ^ (r / 2), so that the 16 rows of one chunk lie in all 64 banks. Lane
+  // at place c ^ (r % 8), so that 8 rows of one chunk fill a 128-byte cycle. Lane
   // (r, g) reads chunk g (first half of the line) or 4 + g.
-  const int xpos0 = r16 * 128 + ((g ^ (r16 >> 1)) << 4), xpos1 = xpos0 ^ 64;
+  const int xpos0 = r16 * 128 + ((g ^ (r16 & 7)) << 4), xpos1 = xpos0 ^ 64;
 
   f4_t acc[RT][NT];
 #pragma unroll
@@ -142,24 +143,34 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     // every wave's and frees the other stage
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(NT * S) : "memory");
     const unsigned char* xb = smem + st * STAGE + wm * RT * REC * 1024;
-    const unsigned char* sb = smem + st * STAGE + XBYTES + (wm * RT * 16 + r16) * 16 + g + (S == 2 ? 8 * (b & 1) : 0);
+    const unsigned char* sb = smem + st * STAGE + XBYTES + wm * RT * 256 + r16 * 4 + g + (S == 2 ? 128 * (b & 1) : 0);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       ws[p] = wsn[p];
-      if (S == 2 && (b & 1)) ws[p] = ws[p] >> 16;
+      if (S == 2) ws[p] = ws[p] >> (16u * (b & 1));
     }
+    static_assert(RT % 2 == 0, "the operand's two places alternate");
+    // X's operand of row tile r and step s, read one row tile ahead of its use
+    i8_t x[2];
+    uint32_t xs[2];
+    auto read_x = [&](int s, int r, int to) {
+      const unsigned char* xl = xb + (r * (REC / 2) + s * XW / 2) * 2048;
+      const u4_t lo = *(const u4_t*)(xl + (XW == 1 && s % 2 ? xpos1 : xpos0));
+      u4_t hi = {0u, 0u, 0u, 0u};
+      if constexpr (XW == 2) hi = *(const u4_t*)(xl + xpos1);
+      x[to] = i8_t{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+      xs[to] = sb[r * 256 + s * 64];
+    };
+    read_x(0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
     auto step = [&](auto sel) {
       constexpr int s = decltype(sel)::value;
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const unsigned char* xl = xb + (r * (REC / 2) + s * XW / 2) * 2048;
-        const u4_t lo = *(const u4_t*)(xl + (XW == 1 && s % 2 ? xpos1 : xpos0));
-        u4_t hi = {0u, 0u, 0u, 0u};
-        if constexpr (XW == 2) hi = *(const u4_t*)(xl + xpos1);
-        const i8_t x = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-        const uint32_t xs = sb[r * 256 + s * 4];
+        if (r + 1 < RT) read_x(s, r + 1, (r + 1) & 1);
+        else if (s + 1 < S) read_x(s + 1, 0, 0);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) acc[r][i] = mfma_mx<FMT, s>(w[s][i], ws[i >> 1][i & 1], x, xs, acc[r][i]);
+        for (int i = 0; i < NT; ++i) acc[r][i] = mfma_mx<FMT, s>(w[s][i], ws[i >> 1][i & 1], x[r & 1], xs[r & 1], acc[r][i]);
         if constexpr (s == 0) {  // the next block's loads to LDS, spread over the first step
 #pragma unroll
           for (int k = r * ITEMS / RT; k < (r + 1) * ITEMS / RT; ++k) dma_item(b + 1, st ^ 1, k);
@@ -167,8 +178,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
             for (int p = 0; p < NP; ++p) wsn[p] = load_ws(b + 1, p);
           }
-          __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
