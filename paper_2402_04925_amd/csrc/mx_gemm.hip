@@ -208,35 +208,36 @@ hipError_t rows_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
 
 }  // namespace
 
-// Microseconds of a product, fitted to 7,000 launches on 400 random sizes (1 to 2048
-// rows, 512 to 32768 outputs, 512 to 16384 of K; 7 to 15% rms): the choice made by
-// them is 1.6% slower than the best of all kernels, tiles and splits on average, 25%
-// at worst. A workgroup takes max(c1, c2 n) per step of K, n workgroups to a CU, e
-// more for each beyond the first; parts are written and read once. What it is for:
-// 8192 x 8192 at 64 rows fp8 takes 16.0 us in the few-row kernel, 16.4 in tiles of 64
-// x 128 over 4 splits and 23 without; 8192 x 28672 53, 37 and 30; 3584 of K x 8192 at
-// 256 rows 11.3 in tiles of 64 x 128, 15.2 of 64 x 256; 14336 x 8192 at 2048 rows 281
-// and 202, but 194 of 128 x 512.
+// Microseconds of a product, fitted to 10,000 launches on 690 random sizes (1 to 2048
+// rows, 512 to 32768 outputs, 512 to 16384 of K; 8 to 13% rms, the few-row kernel up
+// to 17%): the choice made by them is 1.2% slower than the best of all kernels, tiles
+// and splits on average, 17% at the 99th percentile. A workgroup takes max(c1, c2 n)
+// per step of K, n workgroups to a CU, e more for each beyond the first; parts are
+// written and read once. What the choice is for: 8192 x 8192 at 64 rows fp8 takes
+// 16.0 us in the few-row kernel, 16.4 in tiles of 64 x 128 over 4 splits and 22
+// without; 8192 x 28672 55, 36 (2 splits) and 30; 8192 x 8192 x 3584 at 1000 rows 27 in
+// tiles of 64 x 512, 31 of 64 x 128, 38 of 128 x 512; at 2048 rows of 8192 x 14336 203,
+// 287 and 176.
 struct TileCost {
   int kind, bm, bn;
   double start, c1, c2, e, reduce, mb;
 };
 constexpr TileCost kTileFp8[] = {
-    {kMxTiles128x512, 128, 512, 7.3, 0.00, 1.38, 3.9, 6.8, 8.3e6}, {kMxTiles64x512, 64, 512, 4.8, 0.13, 0.67, 2.8, 3.9, 5.4e6},
-    {kMxTiles64x256, 64, 256, 4.4, 0.00, 0.374, 1.3, 3.4, 5.0e6},  {kMxTiles128x256, 128, 256, 5.3, 0.20, 0.67, 1.6, 4.6, 6.3e6},
-    {kMxTiles64x128, 64, 128, 3.7, 0.08, 0.238, 0.9, 3.2, 4.7e6}};
+    {kMxTiles128x512, 128, 512, 8.4, 0.71, 1.12, 1.0, 5.0, 6.7e6}, {kMxTiles64x512, 64, 512, 5.0, 0.00, 0.674, 2.9, 3.4, 5.2e6},
+    {kMxTiles64x256, 64, 256, 4.4, 0.18, 0.354, 1.5, 3.2, 4.8e6},  {kMxTiles128x256, 128, 256, 5.6, 0.04, 0.60, 3.3, 4.4, 6.4e6},
+    {kMxTiles64x128, 64, 128, 3.7, 0.05, 0.230, 0.9, 3.0, 4.4e6}};
 constexpr TileCost kTileFp4[] = {
-    {kMxTiles128x512, 128, 512, 7.8, 0.16, 0.70, 7.0, 6.7, 8.2e6}, {kMxTiles64x512, 64, 512, 4.2, 0.02, 0.535, 2.7, 4.3, 5.6e6},
-    {kMxTiles64x256, 64, 256, 4.0, 0.15, 0.266, 2.0, 3.6, 5.1e6},  {kMxTiles128x256, 128, 256, 5.7, 0.20, 0.42, 2.1, 4.7, 6.6e6},
-    {kMxTiles64x128, 64, 128, 3.4, 0.09, 0.165, 0.9, 3.3, 4.3e6}};
+    {kMxTiles128x512, 128, 512, 8.3, 0.00, 0.676, 8.6, 6.4, 8.5e6}, {kMxTiles64x512, 64, 512, 4.5, 0.00, 0.546, 2.6, 3.8, 5.4e6},
+    {kMxTiles64x256, 64, 256, 4.2, 0.01, 0.257, 2.0, 3.4, 5.2e6},   {kMxTiles128x256, 128, 256, 5.8, 0.35, 0.394, 1.9, 4.9, 7.0e6},
+    {kMxTiles64x128, 64, 128, 3.5, 0.10, 0.163, 1.0, 3.2, 4.6e6}};
 // The few-row kernel: start + n (workgroups to a CU) iter (chunks a wave takes) +
 // wave (waves), by rows up to 16, 32, 64
 struct RowsCost {
   int waves;
   double start, iter, wave;
 };
-constexpr RowsCost kRowsFp8[] = {{16, 2.2, 0.73, 0.24}, {8, 0.8, 2.24, 0.38}, {5, 0.8, 3.5, 0.42}};
-constexpr RowsCost kRowsFp4[] = {{16, 2.2, 0.64, 0.22}, {8, 2.0, 1.41, 0.23}, {10, 2.4, 1.23, 0.49}};
+constexpr RowsCost kRowsFp8[] = {{16, 2.5, 0.49, 0.26}, {8, 0.9, 2.67, 0.27}, {5, 0.9, 3.1, 0.59}};
+constexpr RowsCost kRowsFp4[] = {{16, 2.1, 0.72, 0.25}, {8, 1.8, 1.37, 0.31}, {10, 1.4, 2.78, 0.34}};
 constexpr int kCus = 256;
 // split-K parts of a call take at most this much workspace
 constexpr int64_t kMxPartBytes = (int64_t)64 << 20;
