@@ -338,7 +338,7 @@ typedef enum { TPDQ_MX_FP4 = 0, TPDQ_MX_FP8 = 1 } tpdq_mx_format;
 typedef enum { TPDQ_MX_ROWS = 0, TPDQ_MX_TILED = 1 } tpdq_mx_layout;
 
 /* R and K are positive, K a multiple of 8 (a last block of 8, 16 or 24 elements
- * has zero codes behind them). */
+ * has zero codes behind them) and at most 2^30. */
 typedef struct tpdq_mx {
   void* codes;
   int64_t ld_c;
@@ -376,7 +376,8 @@ tpdq_status tpdq_mx_pack(const tpdq_mx* src, const tpdq_mx* dst, void* stream);
  * y goes to Y [M][ldy] rounded to dtype (then q is NULL), as tpdq_w4a16_gemm and
  * the MLP shards take it, or to q (TPDQ_MX_ROWS, R = M; then Y is NULL), quantized
  * from fp32 as by tpdq_mx_quantize. X, residual [M][ld] and weight [K] are of
- * dtype. residual_out may be residual itself. K a multiple of 8, at most 65536. The
+ * dtype. residual_out and Y may each be X or residual itself (every element is read
+ * before it is written), but not one another. K a multiple of 8, at most 65536. The
  * sum of squares is taken in fp32: rows of magnitudes past 2^63 / sqrt(K) overflow it.
  * Alignment: every pointer 16 B, every leading dimension % 8 == 0.
  */
@@ -387,7 +388,9 @@ tpdq_status tpdq_rmsnorm(const void* X, int64_t ldx, const void* residual, int64
 /*
  * tpdq_mx_gemm - Y = X W^T: X [M][K] (TPDQ_MX_ROWS, fp8 or fp4), w [N][K]
  * (TPDQ_MX_TILED, fp4), fp32 accumulation over all of K, Y [M][ldy] rounded once to
- * dtype (fp16 or bf16). M = X->R, N = w->R, a multiple of 8; X->K == w->K. Alignment:
+ * dtype (fp16 or bf16). With an fp8 X the matrix instruction aligns each 8
+ * consecutive products to the largest of their exponents and drops what lies 13 bits
+ * below it (1e-4 of a typical output); with an fp4 X nothing is dropped. M = X->R, N = w->R, a multiple of 8; X->K == w->K. Alignment:
  * Y 16 B, ldy % 8 == 0. A NaN (a code's or a scale's) in row m of X gives NaN in row
  * m of Y alone, in row n of w in column n alone. Deterministic.
  * Workspace: tpdq_mx_workspace_bytes(0, M, w, NULL) bytes, any content. Calls that

@@ -31,6 +31,7 @@ tpdq_status check_mx(const tpdq_mx* q, const char* name, int layout, bool addres
     return fail(TPDQ_ERR_UNSUPPORTED, "%s: tiled tensors are fp4", name);
   if (q->R <= 0 || q->K <= 0 || q->K % 8)
     return fail(TPDQ_ERR_SHAPE, "%s: R=%d and K=%d must be positive, K a multiple of 8", name, q->R, q->K);
+  if (q->K > (1 << 30)) return fail(TPDQ_ERR_UNSUPPORTED, "%s: K=%d > 2^30", name, q->K);
   const int64_t c = layout == TPDQ_MX_ROWS ? mx_row_codes(q->K, q->format) : mx_tile_codes(q->K);
   const int64_t s = layout == TPDQ_MX_ROWS ? mx_row_scales(q->K) : mx_tile_scales(q->K);
   if (q->ld_c < c || q->ld_s < s)

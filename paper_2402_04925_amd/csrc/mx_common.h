@@ -121,6 +121,12 @@ __device__ __forceinline__ void store_mx8(const float (&v)[8], int k8, int code_
 // 4 .. 7); in its scale word the byte of elements 32 g .. 32 g + 31. Result:
 // lane (m, g) holds outputs 4 g .. 4 g + 3 of X's row m.
 // WSEL: which byte of the weights' scale word.
+// With fp4 on both sides the products enter the fp32 accumulator whole. With fp8
+// the instruction aligns each 8 consecutive products to the largest exponent among
+// them and drops the bits 13 places below it (seen by adding 2^-j to 256: gone from j
+// = 6 on, for the 7 elements beside it and no others): 1e-4 of a typical sum, where
+// the fp8 code itself is good to 2^-4. The exact form, 16-bit operands, has half the
+// rate and would unpack every weight.
 template <int FMT, int WSEL>
 __device__ __forceinline__ f4_t mfma_mx(u4_t w, uint32_t wscale, i8_t x, uint32_t xscale, f4_t acc) {
   i8_t a = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};

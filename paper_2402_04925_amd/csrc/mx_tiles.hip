@@ -1,17 +1,25 @@
 // Product of microscaled (MX) operands with many rows of X on gfx950: the matrix
 // pipe bounds it (mx_gemm.hip has the few-row kernel and the operands' layout).
 //
-// A workgroup of 8 waves (two per SIMD) computes 32 RT rows x 256 outputs (GATED:
-// 128 of the gate and 128 of the up projection); a wave half of the rows and 64 of
-// the outputs, RT x 4 accumulators. K advances a block of 256 bytes of X at a time
-// (fp8 two instruction steps, fp4 four):
+// A workgroup of NW waves computes 16 RT rows x 32 NP NW outputs (GATED: NP = 2, a
+// tile of the gate and one of the up projection per wave), a wave all of the rows,
+// RT x 2 NP accumulators. K advances a block of S instruction steps of 128 at a time:
 //   * X's codes and scales of block b + 1 go from global memory straight to the
-//     other of two LDS stages, laid out as the instruction's operand, while block b
-//     is multiplied; one barrier per block;
+//     other of two LDS stages while block b is multiplied; one barrier per block. A
+//     load takes 8 rows of a 128-byte line; loads laid out as the operand itself, 16
+//     rows of half a line, cost 10 to 25% more time (256 x 8192 x 3584 fp8 13.5 against
+//     11.3 us). In LDS the line's 16-byte chunks are swapped by row, so that neither
+//     these writes nor the operand reads meet a bank twice;
 //   * the weights, as they are tiled the operand itself, go straight to registers:
 //     a step's records are loaded again, for the next block, as soon as its
-//     instructions are issued. Only two waves share a record, and through LDS it
-//     would take a quarter of the LDS reads that bound the loop next.
+//     instructions are issued. No two waves share a record (2 x 4 waves that shared
+//     them and halved the rows took 196 us where 1 x 8 take 170).
+// 8 waves (two per SIMD) with 128 x 512 outputs run 2048 x 14336 x 8192 in 163 to 178
+// us fp8 (2.7 to 2.95 PFLOP/s, a loop of these instructions alone 4.4) and 106 to 114
+// us fp4 (8.1): the matrix pipe is busy 66 and 57% of the clocks at 1.9 GHz, the rest
+// are the block's barrier and the latencies behind it. A barrier in the middle of the
+// block with three stages (186 and 114 us) and operands read two or three row tiles
+// ahead (no change) were not faster. Smaller tiles fill the CUs at fewer rows (plan_mx).
 #include <algorithm>
 
 #include "mx_common.h"
@@ -19,16 +27,15 @@
 namespace tpdq {
 namespace {
 
-template <int DT, int FMT, int RT, int WM, int NP, int NW, int S, bool GATED, bool QUANT>
+template <int DT, int FMT, int RT, int NP, int NW, int S, bool GATED, bool QUANT>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_mx_tiles(MxArgs a) {
   static_assert(!GATED || NP == 2, "a tile of the gate and one of the up projection");
-  constexpr int WN = NW / WM;
   constexpr int NT = 2 * NP;  // operands per wave
   constexpr int XW = FMT == kFp4 ? 1 : 2;      // 64-byte halves of a row's line per step
   constexpr int REC = S * XW;                  // code records (1 KB) of a row tile per block
-  constexpr int BM = 16 * RT * WM;
-  static_assert(BM % 64 == 0 && (RT * WM * REC) % NW == 0 && (S == 2 || S == 4), "whole records, evenly over the waves");
-  constexpr int XREC = RT * WM * REC / NW;     // ... per wave and block
+  constexpr int BM = 16 * RT;
+  static_assert(BM % 64 == 0 && (RT * REC) % NW == 0 && (S == 2 || S == 4), "whole records, evenly over the waves");
+  constexpr int XREC = RT * REC / NW;     // ... per wave and block
   constexpr int SREC = BM / 16;                // scale records (256 B, a chunk's of 16 rows), one per wave
   static_assert(SREC <= NW, "");               // (the same twice where there are more waves)
   constexpr int XBYTES = BM * REC * 64;
@@ -37,7 +44,6 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / WN, wn = wave % WN;
   const int r16 = lane & 15, g = lane >> 4;
   const int nbm = (a.M + BM - 1) / BM;
   const int ks = a.ks;
@@ -47,7 +53,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int tl = lt - kidx * ntl;
   const int bn = tl / nbm;
   const int row0 = (tl - bn * nbm) * BM;
-  const int T0 = GATED ? WN * bn + wn : NP * (WN * bn + wn);  // the wave's first 32-output tile
+  const int T0 = (GATED ? 1 : NP) * (NW * bn + wave);  // the wave's first 32-output tile
   const int steps = (a.K + kMxStep - 1) / kMxStep;
   const int chunks = (a.K + kMxChunk - 1) / kMxChunk;
   const int tiles = (a.N + kMxTile - 1) / kMxTile;
@@ -142,8 +148,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     // weight loads issued after them may be in flight; the barrier publishes
     // every wave's and frees the other stage
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(NT * S) : "memory");
-    const unsigned char* xb = smem + st * STAGE + wm * RT * REC * 1024;
-    const unsigned char* sb = smem + st * STAGE + XBYTES + wm * RT * 256 + r16 * 4 + g + (S == 2 ? 128 * (b & 1) : 0);
+    const unsigned char* xb = smem + st * STAGE;
+    const unsigned char* sb = smem + st * STAGE + XBYTES + r16 * 4 + g + (S == 2 ? 128 * (b & 1) : 0);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       ws[p] = wsn[p];
@@ -200,7 +206,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int m = row0 + (wm * RT + r) * 16 + r16;
+    const int m = row0 + r * 16 + r16;
     if (ks > 1) {  // this split's part, [split][(gate, up)][M][N]
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
@@ -262,16 +268,16 @@ __global__ __launch_bounds__(256) void k_mx_reduce(MxArgs a, int64_t octets, int
     *(u4_t*)(a.Y + m * a.ldy + 8 * k8) = pack8<DT>(v[0]);
 }
 
-template <int DT, int FMT, int RT, int WM, int NP, int NW, int S, bool GATED, bool QUANT>
+template <int DT, int FMT, int RT, int NP, int NW, int S, bool GATED, bool QUANT>
 hipError_t tiles_launch(const MxArgs& a, hipStream_t s) {
-  constexpr int BM = 16 * RT * WM;
+  constexpr int BM = 16 * RT;
   constexpr int lds = 2 * BM * (S * (FMT == kFp4 ? 64 : 128) + 16);
-  auto* k = k_mx_tiles<DT, FMT, RT, WM, NP, NW, S, GATED, QUANT>;
+  auto* k = k_mx_tiles<DT, FMT, RT, NP, NW, S, GATED, QUANT>;
   static std::atomic<uint64_t> done{0};
   hipError_t e = allow_lds((const void*)k, lds, &done);
   if (e != hipSuccess) return e;
   const int tiles = (int)(QUANT && a.ks == 1 ? mx_chunks(a.N) * (kMxChunk / kMxTile) : (a.N + kMxTile - 1) / kMxTile);
-  const int per = (GATED ? 1 : NP) * NW / WM;
+  const int per = (GATED ? 1 : NP) * NW;
   const int64_t grid = (int64_t)((a.M + BM - 1) / BM) * ((tiles + per - 1) / per) * a.ks;
   k<<<dim3((unsigned)grid), dim3(NW * 64), lds, s>>>(a);
   e = hipGetLastError();
@@ -286,14 +292,14 @@ template <int DT, int FMT, bool GATED, bool QUANT>
 hipError_t tiles_pick(const MxArgs& a, int kind, hipStream_t s) {
   constexpr int S2 = FMT == kFp4 ? 4 : 2;  // fp8 at 128 x 512: registers for two steps
   switch (kind) {
-    case kMxTiles128x512: return tiles_launch<DT, FMT, 8, 1, 2, 8, S2, GATED, QUANT>(a, s);
-    case kMxTiles64x512: return tiles_launch<DT, FMT, 4, 1, 2, 8, 4, GATED, QUANT>(a, s);
-    case kMxTiles64x256: return tiles_launch<DT, FMT, 4, 1, 2, 4, 4, GATED, QUANT>(a, s);
+    case kMxTiles128x512: return tiles_launch<DT, FMT, 8, 2, 8, S2, GATED, QUANT>(a, s);
+    case kMxTiles64x512: return tiles_launch<DT, FMT, 4, 2, 8, 4, GATED, QUANT>(a, s);
+    case kMxTiles64x256: return tiles_launch<DT, FMT, 4, 2, 4, 4, GATED, QUANT>(a, s);
   }
   if constexpr (!GATED) {
     switch (kind) {
-      case kMxTiles128x256: return tiles_launch<DT, FMT, 8, 1, 1, 8, 4, GATED, QUANT>(a, s);
-      case kMxTiles64x128: return tiles_launch<DT, FMT, 4, 1, 1, 4, 4, GATED, QUANT>(a, s);
+      case kMxTiles128x256: return tiles_launch<DT, FMT, 8, 1, 8, 4, GATED, QUANT>(a, s);
+      case kMxTiles64x128: return tiles_launch<DT, FMT, 4, 1, 4, 4, GATED, QUANT>(a, s);
     }
   }
   return hipErrorInvalidValue;

@@ -146,6 +146,8 @@ class MxTensor:
     def column_shard(self, rank: int, tp: int) -> "MxTensor":
         """Column-parallel share of a weight (views): outputs [rank*R/tp, ...)."""
         n = self._R // tp
+        if n * tp != self._R or not 0 <= rank < tp:
+            raise ValueError(f"rank {rank} of {tp} has no equal share of {self._R} outputs")
         r0 = rank * n
         if self._layout == MX_TILED:
             if n % _TILE and tp > 1:
@@ -158,6 +160,8 @@ class MxTensor:
     def row_shard(self, rank: int, tp: int) -> "MxTensor":
         """Row-parallel share of a weight (views): inputs [rank*K/tp, ...)."""
         k = self._K // tp
+        if k * tp != self._K or not 0 <= rank < tp:
+            raise ValueError(f"rank {rank} of {tp} has no equal share of {self._K} inputs")
         if k % _CHUNK and tp > 1:
             raise ValueError("a row shard must start and end on multiples of 512 inputs")
         if tp == 1:

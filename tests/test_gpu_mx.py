@@ -347,6 +347,46 @@ def test_product_of_real_layers(fmt, M, N, K):
     assert err.square().mean().sqrt() <= eps_half("bf16") * want.square().mean().sqrt()
 
 
+# ragged sizes (K and N in no whole block, step, chunk or tile) that reach every tile
+# shape, in 16 bits, quantized and gated (tests/test_mx_ref.py checks that they do)
+TILES = [(1155, 8984, 328), (1421, 2976, 456), (223, 8248, 584), (1639, 4632, 1160), (2040, 8184, 1032), (1526, 5400, 904),
+         (43, 40, 2680), (40, 14344, 1160), (30, 4360, 1096)]
+
+
+def some_rows(M, seed):
+    """Edges of the row tiles and random rows."""
+    rng = np.random.default_rng(seed)
+    edges = [r for t in (16, 64, 128) for r in (0, t - 1, t, M // t * t - 1, M // t * t, M - 1)]
+    return np.unique(np.clip(edges + rng.integers(0, M, 24).tolist(), 0, M - 1))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("M,N,K", TILES)
+def test_product_tiles(fmt, M, N, K):
+    dev = u.torch_dev()
+    q, x = quantized(M, K, fmt, M + N + K, dev)
+    w, wv = weight(N, K, N + K, dev)
+    rows = some_rows(M, N)
+    check_product(tpdq.mx_gemm(q, w, torch_dt("bf16"))[rows], x[rows], wv, "bf16", fmt)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("M,N,K", TILES)
+def test_mlp_tiles(gated, fmt, M, N, K):
+    dev = u.torch_dev()
+    N2 = 72
+    q, x = quantized(M, K, fmt, M + N + K, dev)
+    (wu, wuv), (wd, wdv) = weight(N, K, 1, dev), weight(N2, N, 2, dev)
+    wg, wgv = weight(N, K, 3, dev) if gated else (None, None)
+    rows = some_rows(M, N)
+    y = tpdq.mx_mlp_shard(q, wu, wd, torch_dt("bf16"), w_gate=wg)[rows]
+    want, bound = mlp_want(x[rows], wuv, wdv, wgv, fmt)
+    err = np.abs(f64(y) - want)
+    assert (err <= eps_half("bf16") * np.abs(want) + bound).all(), (err / bound).max()
+    assert np.sqrt((err * err).mean()) <= 2.0 ** -6 * np.sqrt((want * want).mean())
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("M", [1, 20, 64, 130, 300])
 def test_product_not_finite(fmt, M):

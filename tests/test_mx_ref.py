@@ -55,6 +55,26 @@ def test_tiled_places_every_code_once():
     assert (s == 9).sum() == N * 5 and (s != 0).sum() == N * 5
 
 
+def test_the_gpu_tests_reach_every_kernel(lib):
+    """The products that tests/test_gpu_mx.py runs, by the kernel that is planned for
+    them: every tile shape in 16 bits, quantized and gated, and splits of K."""
+    from tests import test_gpu_mx as t
+    plan = getattr(lib, "_ZN4tpdq7plan_mxEiiiibb")  # MxPlan plan_mx(M, N, K, fmt, gated, quant)
+    plan.restype, plan.argtypes = ctypes.c_int64, [ctypes.c_int] * 4 + [ctypes.c_bool] * 2
+    rows, half, t128x512, t64x512, t64x256, t128x256, t64x128 = range(7)
+    for fmt in (ref.FP4, ref.FP8):
+        seen = {}
+        for gated, quant in ((False, False), (False, True), (True, True)):
+            for M, N, K in t.TILES + ([] if quant else t.SHAPES + t.LARGE):
+                p = plan(M, N, K, fmt, gated, quant)
+                seen.setdefault((gated, quant), set()).add((p & 0xFFFFFFFF, (p >> 32) > 1))
+        tiles = {t128x512, t64x512, t64x256, t128x256, t64x128}
+        assert {k for k, _ in seen[False, False]} == tiles | {rows, half}
+        assert {k for k, _ in seen[False, True]} == tiles | {rows}
+        assert {k for k, _ in seen[True, True]} == {t128x512, t64x512, t64x256, rows}
+        assert any(split for _, split in seen[False, False]) and any(split for _, split in seen[True, True])
+
+
 # ---- refusals ------------------------------------------------------------
 
 @pytest.fixture(scope="module")
@@ -164,6 +184,8 @@ def test_product_refusals(lib):
     assert f(Y=(1 << 30) + 8) == _abi.ERR_ALIGN and f(ldy=68) == _abi.ERR_ALIGN
     assert f(x=rows(R=1 << 23)) == _abi.ERR_UNSUPPORTED                          # 2 GiB of codes
     assert f(x=rows(ld_c=1 << 31, R=1)) == _abi.ERR_UNSUPPORTED
+    big = (1 << 30) + 8
+    assert f(x=rows(R=1, K=big), w=tiled(K=big)) == _abi.ERR_UNSUPPORTED         # longer rows than any call takes
     assert f(w=tiled(ld_c=1 << 30)) == _abi.ERR_UNSUPPORTED
 
 
@@ -202,6 +224,8 @@ def test_binding_refuses_on_the_host():
         w.column_shard(0, 2)                                  # 48 rows: no whole tiles
     with pytest.raises(ValueError):
         w.row_shard(0, 2)                                     # 768 inputs: no whole chunks
+    with pytest.raises(ValueError):
+        w.column_shard(0, 5)                                  # 96 / 5
     with pytest.raises(ValueError):
         w.scales
     assert w.row_shard(1, 3).codes.shape == (3, 4 * 2048) and w.row_shard(1, 3).padded_scales.shape == (3, 512)
