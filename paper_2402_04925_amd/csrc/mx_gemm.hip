@@ -186,7 +186,7 @@ hipError_t rows_launch(const MxArgs& a, hipStream_t s) {
 
 template <int DT, int FMT, bool GATED, bool QUANT>
 hipError_t rows_pick(const MxArgs& a, int kind, hipStream_t s) {
-  constexpr int NW4 = FMT == kFp4 ? 10 : 5;  // what LDS holds of 64 rows
+  constexpr int NW4 = FMT == kFp8 ? 5 : GATED ? 8 : 10;  // what LDS, or registers, hold of 64 rows
   if constexpr (!GATED && !QUANT) {
     if (kind == kMxRowsHalf) {
       if (a.M <= 16) return rows_launch<DT, FMT, 1, 1, GATED, QUANT, 16>(a, s);
