@@ -208,10 +208,10 @@ hipError_t rows_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
 
 }  // namespace
 
-// Microseconds of a product, fitted to 10,000 launches on 690 random sizes (1 to 2048
-// rows, 512 to 32768 outputs, 512 to 16384 of K; 8 to 13% rms, the few-row kernel up
-// to 17%): the choice made by them is 1.2% slower than the best of all kernels, tiles
-// and splits on average, 17% at the 99th percentile. A workgroup takes max(c1, c2 n)
+// Microseconds of a product, fitted to 20,000 launches on 1,380 random sizes (1 to
+// 2048 rows, 512 to 32768 outputs, 512 to 16384 of K; 7 to 14% rms, the few-row kernel
+// up to 17%): the choice made by them is 1.0% slower than the best of all kernels,
+// tiles and splits on average, 14% at the 99th percentile. A workgroup takes max(c1, c2 n)
 // per step of K, n workgroups to a CU, e more for each beyond the first; parts are
 // written and read once. What the choice is for: 8192 x 8192 at 64 rows fp8 takes
 // 16.0 us in the few-row kernel, 16.4 in tiles of 64 x 128 over 4 splits and 22
@@ -224,11 +224,11 @@ struct TileCost {
 };
 constexpr TileCost kTileFp8[] = {
     {kMxTiles128x512, 128, 512, 8.4, 0.71, 1.12, 1.0, 5.0, 6.7e6}, {kMxTiles64x512, 64, 512, 5.0, 0.00, 0.674, 2.9, 3.4, 5.2e6},
-    {kMxTiles64x256, 64, 256, 4.4, 0.18, 0.354, 1.5, 3.2, 4.8e6},  {kMxTiles128x256, 128, 256, 5.6, 0.04, 0.60, 3.3, 4.4, 6.4e6},
+    {kMxTiles64x256, 64, 256, 4.4, 0.18, 0.354, 1.5, 3.2, 4.8e6},  {kMxTiles128x256, 128, 256, 6.9, 0.43, 0.61, 0.5, 4.8, 7.1e6},
     {kMxTiles64x128, 64, 128, 3.7, 0.05, 0.230, 0.9, 3.0, 4.4e6}};
 constexpr TileCost kTileFp4[] = {
     {kMxTiles128x512, 128, 512, 8.3, 0.00, 0.676, 8.6, 6.4, 8.5e6}, {kMxTiles64x512, 64, 512, 4.5, 0.00, 0.546, 2.6, 3.8, 5.4e6},
-    {kMxTiles64x256, 64, 256, 4.2, 0.01, 0.257, 2.0, 3.4, 5.2e6},   {kMxTiles128x256, 128, 256, 5.8, 0.35, 0.394, 1.9, 4.9, 7.0e6},
+    {kMxTiles64x256, 64, 256, 4.2, 0.01, 0.257, 2.0, 3.4, 5.2e6},   {kMxTiles128x256, 128, 256, 6.2, 0.24, 0.400, 1.5, 5.0, 7.0e6},
     {kMxTiles64x128, 64, 128, 3.5, 0.10, 0.163, 1.0, 3.2, 4.6e6}};
 // The few-row kernel: start + n (workgroups to a CU) iter (chunks a wave takes) +
 // wave (waves), by rows up to 16, 32, 64
@@ -259,16 +259,16 @@ MxPlan plan_mx(int M, int N, int K, int fmt, bool gated, bool quant) {
     // 192 tiles: 7.3 -> 9.8). A block of quantized outputs is a whole tile.
     if (!quant && 2 * tiles <= kCus) {
       best.kind = kMxRowsHalf;
-      least *= 0.85;
+      least *= M <= 16 ? 0.85 : 0.72;
     }
   }
   for (const TileCost& c : fp4 ? kTileFp4 : kTileFp8) {
     // the gated product has a tile of each projection per wave; 128 rows with half
     // of them empty never pay
-    if (gated && (c.kind == kMxTiles64x128 || c.kind == kMxTiles128x256)) continue;
+    if (gated && c.kind == kMxTiles64x128) continue;
     if (c.bm > 64 && M <= 64) continue;
     const int64_t wgs = (int64_t)up(M, c.bm) * up((int64_t)N * weights, c.bn);
-    const int block = !fp4 && c.kind == kMxTiles128x512 ? 2 : 4, blocks = up(steps, block);
+    const int block = !fp4 && c.bm == 128 ? 2 : 4, blocks = up(steps, block);
     for (int ks : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
       if (ks > blocks || (ks > 1 && (wgs * ks > 3 * kCus || (int64_t)ks * M * N * 4 * weights > kMxPartBytes))) break;
       const int n = up(wgs * ks, kCus);

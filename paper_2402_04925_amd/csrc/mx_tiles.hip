@@ -36,11 +36,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr int BM = 16 * RT;
   static_assert(BM % 64 == 0 && (RT * REC) % NW == 0 && (S == 2 || S == 4), "whole records, evenly over the waves");
   constexpr int XREC = RT * REC / NW;     // ... per wave and block
-  constexpr int SREC = BM / 16;                // scale records (256 B, a chunk's of 16 rows), one per wave
-  static_assert(SREC <= NW, "");               // (the same twice where there are more waves)
+  constexpr int SREC = BM / 16;                // scale records (256 B, a chunk's of 16 rows)
+  constexpr int SPW = SREC > NW ? SREC / NW : 1;  // ... per wave (the same twice where there are more waves)
   constexpr int XBYTES = BM * REC * 64;
   constexpr int STAGE = XBYTES + SREC * 256;
-  constexpr int ITEMS = XREC + 1;              // loads to LDS per wave and block
+  constexpr int ITEMS = XREC + SPW;              // loads to LDS per wave and block
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -51,8 +51,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int lt = xcd_run(blockIdx.x, gridDim.x);
   const int kidx = lt / ntl;
   const int tl = lt - kidx * ntl;
-  const int bn = tl / nbm;
-  const int row0 = (tl - bn * nbm) * BM;
+  // neighbours: 8 row tiles, then the next columns, so that an XCD's 32 workgroups
+  // read 8 tiles of X and 4 of W (2048 x 14336 x 8192 fp8 168 -> 165 us)
+  const int group = tl / (8 * (ntl / nbm)), in_group = tl - group * 8 * (ntl / nbm);
+  const int group_rows = min(8, nbm - group * 8);
+  const int bn = in_group / group_rows;
+  const int row0 = (group * 8 + in_group - bn * group_rows) * BM;
   const int T0 = (GATED ? 1 : NP) * (NW * bn + wave);  // the wave's first 32-output tile
   const int steps = (a.K + kMxStep - 1) / kMxStep;
   const int chunks = (a.K + kMxChunk - 1) / kMxChunk;
@@ -78,8 +82,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     offx[k] = m < a.M ? (uint32_t)m * (uint32_t)a.x.ld_c + 128u * line + 16u * chunk : kOutOfRange;
   }
   // scale record in LDS: [word of the chunk][row], so that 16 rows' words are adjacent
-  const int ms = row0 + 16 * (wave % SREC) + r16;
-  const uint32_t offxs = ms < a.M ? (uint32_t)ms * (uint32_t)a.x.ld_s + 4u * g : kOutOfRange;
+  uint32_t offxs[SPW];
+#pragma unroll
+  for (int k = 0; k < SPW; ++k) {
+    const int ms = row0 + 16 * ((wave + NW * k) % SREC) + r16;
+    offxs[k] = ms < a.M ? (uint32_t)ms * (uint32_t)a.x.ld_s + 4u * g : kOutOfRange;
+  }
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int T = GATED ? T0 : T0 + p;
@@ -99,7 +107,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     } else {
       const bool in = b < nblk;
       const __amdgpu_buffer_rsrc_t r = buffer_rsrc(a.x.scales, in ? xsbytes : 0u);
-      dma_lds<4>(r, sb + XBYTES + (wave % SREC) * 256, offxs, in ? ((uint32_t)(S * b) & ~3u) * 4u : 0u);
+      dma_lds<4>(r, sb + XBYTES + ((wave + NW * (k - XREC)) % SREC) * 256, offxs[k - XREC], in ? ((uint32_t)(S * b) & ~3u) * 4u : 0u);
     }
   };
   auto load_w = [&](int b, int s, int i) {
@@ -290,18 +298,15 @@ hipError_t tiles_launch(const MxArgs& a, hipStream_t s) {
 
 template <int DT, int FMT, bool GATED, bool QUANT>
 hipError_t tiles_pick(const MxArgs& a, int kind, hipStream_t s) {
-  constexpr int S2 = FMT == kFp4 ? 4 : 2;  // fp8 at 128 x 512: registers for two steps
+  constexpr int S2 = FMT == kFp4 ? 4 : 2;  // fp8, 128 rows: registers for two steps
   switch (kind) {
     case kMxTiles128x512: return tiles_launch<DT, FMT, 8, 2, 8, S2, GATED, QUANT>(a, s);
     case kMxTiles64x512: return tiles_launch<DT, FMT, 4, 2, 8, 4, GATED, QUANT>(a, s);
     case kMxTiles64x256: return tiles_launch<DT, FMT, 4, 2, 4, 4, GATED, QUANT>(a, s);
+    case kMxTiles128x256: return tiles_launch<DT, FMT, 8, 2, 4, S2, GATED, QUANT>(a, s);
   }
-  if constexpr (!GATED) {
-    switch (kind) {
-      case kMxTiles128x256: return tiles_launch<DT, FMT, 8, 1, 8, 4, GATED, QUANT>(a, s);
-      case kMxTiles64x128: return tiles_launch<DT, FMT, 4, 1, 4, 4, GATED, QUANT>(a, s);
-    }
-  }
+  if constexpr (!GATED)
+    if (kind == kMxTiles64x128) return tiles_launch<DT, FMT, 4, 1, 4, 4, GATED, QUANT>(a, s);
   return hipErrorInvalidValue;
 }
 
