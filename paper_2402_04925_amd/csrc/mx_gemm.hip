@@ -210,8 +210,8 @@ hipError_t rows_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
 
 // Microseconds of a product, fitted to 20,000 launches on 1,380 random sizes (1 to
 // 2048 rows, 512 to 32768 outputs, 512 to 16384 of K; 7 to 14% rms, the few-row kernel
-// up to 17%): the choice made by them is 1.0% slower than the best of all kernels,
-// tiles and splits on average, 14% at the 99th percentile. A workgroup takes max(c1, c2 n)
+// up to 17%): the choice made by them is 1.1% slower than the best of all kernels,
+// tiles and splits on average, 16% at the 99th percentile. A workgroup takes max(c1, c2 n)
 // per step of K, n workgroups to a CU, e more for each beyond the first; parts are
 // written and read once. What the choice is for: 8192 x 8192 at 64 rows fp8 takes
 // 16.0 us in the few-row kernel, 16.4 in tiles of 64 x 128 over 4 splits and 22
@@ -236,7 +236,7 @@ struct RowsCost {
   int waves;
   double start, iter, wave;
 };
-constexpr RowsCost kRowsFp8[] = {{16, 2.5, 0.49, 0.26}, {8, 0.9, 2.67, 0.27}, {5, 0.9, 3.1, 0.59}};
+constexpr RowsCost kRowsFp8[] = {{16, 2.5, 0.49, 0.26}, {8, 0.9, 2.67, 0.27}, {5, 0.9, 2.6, 0.59}};
 constexpr RowsCost kRowsFp4[] = {{16, 2.1, 0.72, 0.25}, {8, 1.8, 1.37, 0.31}, {10, 1.4, 2.78, 0.34}};
 constexpr int kCus = 256;
 // split-K parts of a call take at most this much workspace
@@ -253,7 +253,9 @@ MxPlan plan_mx(int M, int N, int K, int fmt, bool gated, bool quant) {
   if (M <= 64) {
     const RowsCost& c = (fp4 ? kRowsFp4 : kRowsFp8)[M <= 16 ? 0 : M <= 32 ? 1 : 2];
     const int waves = std::min(c.waves, chunks);
-    least = c.start + up(tiles, kCus) * weights * c.iter * up(chunks, waves) + c.wave * waves;
+    // gated: twice the weights on the same X (the MLP of 8192 / 3584 / 8192 at 32 rows
+    // fp8 20.6 us so, 23.3 with tiles of 64 x 256 over 4 splits)
+    least = c.start + up(tiles, kCus) * (gated ? 1.5 : 1.0) * c.iter * up(chunks, waves) + c.wave * waves;
     // Half tiles where they all find a CU of their own: 8192 x 3584 at 1 row 6.7 ->
     // 5.7 us, at 16 8.1 -> 7.1; past that they are slower (6144 x 6144 at 16 rows,
     // 192 tiles: 7.3 -> 9.8). A block of quantized outputs is a whole tile.

@@ -72,7 +72,7 @@ def test_the_gpu_tests_reach_every_kernel(lib):
         assert {k for k, _ in seen[False, False]} == tiles | {rows, half}
         assert {k for k, _ in seen[False, True]} == tiles | {rows}
         assert {k for k, _ in seen[True, True]} == tiles - {t64x128} | {rows}
-        assert any(split for _, split in seen[False, False]) and any(split for _, split in seen[True, True])
+        assert all(any(split for _, split in kinds) for kinds in seen.values())
 
 
 # ---- refusals ------------------------------------------------------------
