@@ -78,9 +78,21 @@ class MxTensor:
                 or s.dtype is not torch.float8_e8m0fnu or c.shape[0] != rows or s.shape[0] != rows):
             raise ValueError("codes (float8_e4m3fn for fp8, uint8 for fp4) and padded_scales (float8_e8m0fnu) must be 2-D "
                              "with unit column stride, on one device, a row for each row (tiled: each 32)")
+        # the C ABI sees the leading dimensions alone: columns cut short may end past the storage
+        per_c, per_s = self._widths(fmt, layout)
+        if c.shape[1] < _up(K, _STEP) * per_c or s.shape[1] < _up(K, _CHUNK) * per_s:
+            raise ValueError(f"rows of {c.shape[1]} bytes of codes and {s.shape[1]} scales are shorter than K={K} padded to "
+                             f"whole steps and chunks")
         # one row has whatever stride: its leading dimension is its length
         self._set(c, s, R, K, fmt, layout, dev, c.stride(0) if rows > 1 else c.shape[1],
                   s.stride(0) if rows > 1 else s.shape[1])
+
+    @staticmethod
+    def _widths(fmt, layout):
+        """Bytes of a row (of a tile): of codes per step, of scales per chunk."""
+        if fmt not in (MX_FP4, MX_FP8):
+            raise ValueError(f"unknown format {fmt}")
+        return (2048, 512) if layout == MX_TILED else (64 if fmt == MX_FP4 else 128, 16)
 
     def _set(self, c, s, R, K, fmt, layout, dev, ld_c, ld_s):
         self._codes, self._scales, self._R, self._K, self._fmt, self._layout, self._device = c, s, R, K, fmt, layout, dev
@@ -99,16 +111,10 @@ class MxTensor:
     def empty(cls, R: int, K: int, fmt: int, device, layout: int = MX_ROWS) -> "MxTensor":
         """Storage for mx_quantize, rmsnorm or mx_pack to write."""
         torch = _torch()
-        steps, chunks = -(-K // _STEP), -(-K // _CHUNK)
-        if fmt == MX_FP8:
-            t, c = torch.float8_e4m3fn, steps * 128
-        elif fmt == MX_FP4:
-            t, c = torch.uint8, steps * 64
-        else:
-            raise ValueError(f"unknown format {fmt}")
-        rows, s = R, chunks * 16
-        if layout == MX_TILED:
-            rows, c, s = _up(R, _TILE), steps * 2048, chunks * 512
+        per_c, per_s = cls._widths(fmt, layout)
+        c, s = -(-K // _STEP) * per_c, -(-K // _CHUNK) * per_s
+        t = torch.float8_e4m3fn if fmt == MX_FP8 else torch.uint8
+        rows = -(-R // _TILE) if layout == MX_TILED else R
         q = cls.__new__(cls)
         codes = torch.empty((rows, c), dtype=t, device=device)
         q._set(codes, torch.empty((rows, s), dtype=torch.float8_e8m0fnu, device=device), R, K, fmt, layout, codes.device,
@@ -167,7 +173,7 @@ class MxTensor:
         if tp == 1:
             return self
         steps, chunks = k // _STEP, k // _CHUNK
-        per_c, per_s = (2048, 512) if self._layout == MX_TILED else (64 if self._fmt == MX_FP4 else 128, 16)
+        per_c, per_s = self._widths(self._fmt, self._layout)
         return MxTensor(self._codes[:, rank * steps * per_c:(rank + 1) * steps * per_c],
                         self._scales[:, rank * chunks * per_s:(rank + 1) * chunks * per_s],
                         self._R, k, self._fmt, self._layout)

@@ -231,3 +231,22 @@ def test_binding_refuses_on_the_host():
     assert w.row_shard(1, 3).codes.shape == (3, 4 * 2048) and w.row_shard(1, 3).padded_scales.shape == (3, 512)
     with pytest.raises(ValueError):
         tpdq.mx_gemm(tpdq.MxTensor.empty(1, 1536, tpdq.MX_FP8, "cpu"), w, torch.float16)
+
+
+@pytest.mark.parametrize("fmt,layout", [(_abi.MX_FP4, _abi.MX_ROWS), (_abi.MX_FP8, _abi.MX_ROWS), (_abi.MX_FP4, _abi.MX_TILED)])
+def test_views_cut_short_are_no_tensor(fmt, layout):
+    """The leading dimension of a cut view is the whole row's: a call would read past
+    the last row's end."""
+    import torch
+    import paper_2402_04925_amd as tpdq
+    q = tpdq.MxTensor.empty(64, 1024, fmt, "cpu", layout)
+    c, s = q.codes, q.padded_scales
+    make = lambda c, s, K: tpdq.MxTensor(c, s, 64, K, fmt, layout)
+    half_c, half_s = c.shape[1] // 2, s.shape[1] // 2
+    assert make(c[:, half_c:], s[:, half_s:], 512).K == 512
+    assert make(c[:, 16:], s, 896).K == 896
+    for bad in ((c[:, half_c:], s, 1024), (c, s[:, half_s:], 1024), (c[:, 16:], s, 1024), (c[:, half_c:], s[:, half_s:], 520)):
+        with pytest.raises(ValueError):
+            make(*bad)
+    with pytest.raises(ValueError):
+        tpdq.MxTensor(c, s, 64, 1024, 2, layout)
