@@ -56,10 +56,12 @@ tpdq_status check_rows16(const void* p, int64_t ld, int64_t K, const char* name)
 
 MxRows rows_of(const tpdq_mx* q) { return MxRows{(uint8_t*)q->codes, q->ld_c, (uint8_t*)q->scales, q->ld_s}; }
 
-// A launch has fewer than 2^32 threads; the row-wise kernels and mx_pack take one
-// for 32 elements of rows padded to whole chunks (large calls).
+// A launch has fewer than 2^32 threads. Large calls take one for 32 elements: 16 for
+// a chunk of a row, four rows (mx_pack: 32) together, and the chunks of a row in whole
+// workgroups of at most four.
 tpdq_status check_grid(int64_t R, int64_t K) {
-  if (R * mx_chunks(K) >= (int64_t)1 << 28)
+  const int64_t chunks = mx_chunks(K), seg = (chunks + 3) / 4;
+  if ((R + kMxTile) * (seg * ((chunks + seg - 1) / seg)) >= (int64_t)1 << 28)
     return fail(TPDQ_ERR_UNSUPPORTED, "%lld rows of %lld: more threads than a launch has, split the rows", (long long)R,
                 (long long)K);
   return TPDQ_OK;
@@ -173,6 +175,7 @@ tpdq_status tpdq_rmsnorm(const void* X, int64_t ldx, const void* residual, int64
     if (st != TPDQ_OK) return st;
   }
   if ((Y == nullptr) == (q == nullptr)) return fail(TPDQ_ERR_NULL, "one of Y and q is given");
+  if (Y && Y == residual_out) return fail(TPDQ_ERR_SHAPE, "Y and residual_out are the same memory");
   if (Y) {
     st = check_rows16(Y, ldy, K, "Y");
   } else {

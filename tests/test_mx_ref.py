@@ -133,6 +133,9 @@ def test_quantize_refusals(lib):
     assert f(X=(1 << 30) + 8) == _abi.ERR_ALIGN and f(ldx=260) == _abi.ERR_ALIGN
     assert f(t=rows(R=1 << 30, K=8192)) == _abi.ERR_SHAPE  # ldx < K
     assert f(t=rows(R=1 << 30, K=8192), ldx=8192) == _abi.ERR_UNSUPPORTED
+    # five chunks of a row are two workgroups of three waves: 2^32 threads from 2^28 / 6 rows on
+    assert f(t=rows(R=(1 << 28) // 5 - 1, K=2056), ldx=2056) == _abi.ERR_UNSUPPORTED
+    assert f(t=rows(R=(1 << 28) - 1, K=8), ldx=8) == _abi.ERR_UNSUPPORTED
     g = lambda X=1 << 30, ldx=256, dt=0: lib.tpdq_mx_dequantize(ref_of(q), dt, X, ldx, None)
     assert g(X=None) == _abi.ERR_NULL and g(ldx=128) == _abi.ERR_SHAPE and g(dt=-1) == _abi.ERR_SHAPE
     assert g(X=(1 << 30) + 2) == _abi.ERR_ALIGN
@@ -168,6 +171,7 @@ def test_rmsnorm_refusals(lib):
     assert f(ldx=260) == _abi.ERR_ALIGN and f(w=(1 << 31) + 8) == _abi.ERR_ALIGN and f(Y=(1 << 32) + 8) == _abi.ERR_ALIGN
     r = dict(res=1 << 33, h=1 << 34)
     assert f(**r, ldr=128) == _abi.ERR_SHAPE and f(**r, ldh=128) == _abi.ERR_SHAPE and f(**r, ldr=260) == _abi.ERR_ALIGN
+    assert f(**{**r, "h": 1 << 32}) == _abi.ERR_SHAPE                             # Y and residual_out are one
     big = dict(M=1 << 22, K=8192, ldx=8192, ldy=8192)
     assert f(**big) == _abi.ERR_UNSUPPORTED                                       # 2^32 threads
     assert f(Y=None, q=rows(R=5)) == _abi.ERR_SHAPE and f(Y=None, q=rows(K=384)) == _abi.ERR_SHAPE
