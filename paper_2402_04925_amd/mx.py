@@ -46,6 +46,11 @@ def _same_device(device, name, t):
         raise ValueError(f"{name} is on {t.device}, X on {device}")
 
 
+def _ld(t):
+    """Leading dimension of a matrix; one row has whatever stride, and is its length apart."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
 def _rows16(name, t, M=None, K=None, dtype=None):
     """A 16-bit matrix with unit column stride (M x K, of dtype)."""
     if t.dim() != 2 or t.stride(1) != 1:
@@ -83,9 +88,7 @@ class MxTensor:
         if c.shape[1] < _up(K, _STEP) * per_c or s.shape[1] < _up(K, _CHUNK) * per_s:
             raise ValueError(f"rows of {c.shape[1]} bytes of codes and {s.shape[1]} scales are shorter than K={K} padded to "
                              f"whole steps and chunks")
-        # one row has whatever stride: its leading dimension is its length
-        self._set(c, s, R, K, fmt, layout, dev, c.stride(0) if rows > 1 else c.shape[1],
-                  s.stride(0) if rows > 1 else s.shape[1])
+        self._set(c, s, R, K, fmt, layout, dev, _ld(c), _ld(s))
 
     @staticmethod
     def _widths(fmt, layout):
@@ -203,7 +206,7 @@ def mx_quantize(X, fmt: int, out: Optional[MxTensor] = None) -> MxTensor:
     _rows16("X", X)
     dev = _device_of("X", X)
     out = _mx_out(out, X.shape[0], X.shape[1], fmt, dev)
-    _run(dev, _abi.lib().tpdq_mx_quantize, X.data_ptr(), X.stride(0), _dtype_code(X.dtype), out._ref)
+    _run(dev, _abi.lib().tpdq_mx_quantize, X.data_ptr(), _ld(X), _dtype_code(X.dtype), out._ref)
     return out
 
 
@@ -217,7 +220,7 @@ def mx_dequantize(q: MxTensor, dtype, out=None):
     else:
         _rows16("out", out, q._R, q._K, dtype)
         _same_device(dev, "out", out)
-    _run(dev, _abi.lib().tpdq_mx_dequantize, ref, code, out.data_ptr(), out.stride(0))
+    _run(dev, _abi.lib().tpdq_mx_dequantize, ref, code, out.data_ptr(), _ld(out))
     return out
 
 
@@ -253,7 +256,7 @@ def rmsnorm(X, weight, eps: float, residual=None, fmt: Optional[int] = None, res
             h = residual_out
             _rows16("residual_out", h, M, K, dt)
             _same_device(dev, "residual_out", h)
-        res, ldr, hp, ldh = residual.data_ptr(), residual.stride(0), h.data_ptr(), h.stride(0)
+        res, ldr, hp, ldh = residual.data_ptr(), _ld(residual), h.data_ptr(), _ld(h)
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
     if fmt is None:
@@ -262,11 +265,11 @@ def rmsnorm(X, weight, eps: float, residual=None, fmt: Optional[int] = None, res
         else:
             _rows16("out", out, M, K, dt)
             _same_device(dev, "out", out)
-        y, ldy, ref = out.data_ptr(), out.stride(0), None
+        y, ldy, ref = out.data_ptr(), _ld(out), None
     else:
         out = _mx_out(out, M, K, fmt, dev)
         y, ldy, ref = None, 0, out._ref
-    _run(dev, _abi.lib().tpdq_rmsnorm, X.data_ptr(), X.stride(0), res, ldr, weight.data_ptr(), eps, M, K, code, hp, ldh,
+    _run(dev, _abi.lib().tpdq_rmsnorm, X.data_ptr(), _ld(X), res, ldr, weight.data_ptr(), eps, M, K, code, hp, ldh,
          y, ldy, ref)
     return out, h
 
@@ -306,7 +309,7 @@ def mx_gemm(X: MxTensor, w: MxTensor, dtype, out=None, workspace: Optional[Works
     code = _dtype_code(dtype)
     out = _out16(out, X._R, w._R, dtype, dev)
     ws, nbytes, _buf = _scratch(workspace, _workspace_bytes(_abi.OP_MX_GEMM, X._R, w._R, w._K, 0), dev)
-    _run(dev, _abi.lib().tpdq_mx_gemm, cx, cw, code, out.data_ptr(), out.stride(0), ws, nbytes)
+    _run(dev, _abi.lib().tpdq_mx_gemm, cx, cw, code, out.data_ptr(), _ld(out), ws, nbytes)
     return out
 
 

@@ -577,6 +577,28 @@ def test_two_streams_at_once():
         assert all(torch.equal(y, want[i]) for y in got[i])
 
 
+def test_one_row_of_whatever_stride():
+    """torch keeps any stride for an axis of one: a row of a wider buffer, a turned column."""
+    import torch
+    dev = u.torch_dev()
+    K, N = 520, 72
+    x = acts(1, K, 1, dev, "bf16")
+    nw = torch.ones(K, dtype=torch.bfloat16, device=dev)
+    w, _ = weight(N, K, 2, dev)
+    q = tpdq.mx_quantize(x, tpdq.MX_FP8)
+    y, h = tpdq.rmsnorm(x, nw, 1e-5, residual=x)
+    for ld in (1, 3, K + 4):
+        turned = lambda n: torch.empty(max(n, ld), dtype=torch.bfloat16, device=dev).as_strided((1, n), (ld, 1))
+        xt, out = turned(K), turned(N)
+        xt.copy_(x)
+        qt = tpdq.mx_quantize(xt, tpdq.MX_FP8)
+        assert torch.equal(qt.codes.view(torch.uint8), q.codes.view(torch.uint8))
+        assert torch.equal(tpdq.mx_dequantize(q, torch.bfloat16, out=turned(K)), tpdq.mx_dequantize(q, torch.bfloat16))
+        yt, ht = tpdq.rmsnorm(xt, nw, 1e-5, residual=xt, residual_out=turned(K), out=turned(K))
+        assert torch.equal(yt, y) and torch.equal(ht, h)
+        assert torch.equal(tpdq.mx_gemm(q, w, torch.bfloat16, out=out), tpdq.mx_gemm(q, w, torch.bfloat16))
+
+
 def test_binding_refuses():
     import torch
     dev = u.torch_dev()
