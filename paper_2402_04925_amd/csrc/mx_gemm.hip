@@ -214,10 +214,10 @@ hipError_t rows_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
 // tiles and splits on average, 16% at the 99th percentile. A workgroup takes max(c1, c2 n)
 // per step of K, n workgroups to a CU, e more for each beyond the first; parts are
 // written and read once. What the choice is for: 8192 x 8192 at 64 rows fp8 takes
-// 16.0 us in the few-row kernel, 16.4 in tiles of 64 x 128 over 4 splits and 22
-// without; 8192 x 28672 55, 36 (2 splits) and 30; 8192 x 8192 x 3584 at 1000 rows 27 in
-// tiles of 64 x 512, 31 of 64 x 128, 38 of 128 x 512; at 2048 rows of 8192 x 14336 203,
-// 287 and 176.
+// 15.9 us in the few-row kernel, 16.4 in tiles of 64 x 128 over 4 splits and 22.9
+// without; 28672 outputs there 55, 36 (2 splits) and 30; 8192 outputs of K 3584 at 1000
+// rows 28 in tiles of 64 x 512, 32 of 64 x 128, 41 of 128 x 512; 14336 of K 8192 at 2048
+// rows 204, 230 and 172.
 struct TileCost {
   int kind, bm, bn;
   double start, c1, c2, e, reduce, mb;
@@ -276,6 +276,9 @@ MxPlan plan_mx(int M, int N, int K, int fmt, bool gated, bool quant) {
       const int n = up(wgs * ks, kCus);
       double t = c.start + (double)(up(blocks, ks) * block) * std::max(c.c1, c.c2 * n) + c.e * (n - 1);
       if (ks > 1) t += c.reduce + (double)ks * M * N * weights * 8 / c.mb;
+      // (3,000 gated launches: the choice 1.1% from the best so, 1.4 without; the first
+      // product of 8192 / 3584 / 8192 at 1000 rows 53.5 us here, 49.3 in tiles of 64 x 512)
+      if (gated && c.kind == kMxTiles128x256) t *= 1.06;
       if (t < least) {
         least = t;
         best = MxPlan{c.kind, ks};

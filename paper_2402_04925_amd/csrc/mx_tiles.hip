@@ -18,8 +18,9 @@
 // us fp8 (2.7 to 2.95 PFLOP/s, a loop of these instructions alone 4.4) and 106 to 114
 // us fp4 (8.1): the matrix pipe is busy 66 and 57% of the clocks at 1.9 GHz, the rest
 // are the block's barrier and the latencies behind it. A barrier in the middle of the
-// block with three stages (186 and 114 us) and operands read two or three row tiles
-// ahead (no change) were not faster. Smaller tiles fill the CUs at fewer rows (plan_mx).
+// block with three stages (171 and 113 us where this took 165 and 106) and operands
+// read two or three row tiles ahead (no change) were not faster. Smaller tiles fill
+// the CUs at fewer rows (plan_mx).
 #include <algorithm>
 
 #include "mx_common.h"
