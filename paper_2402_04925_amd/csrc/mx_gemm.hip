@@ -212,24 +212,33 @@ hipError_t rows_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
 // 2048 rows, 512 to 32768 outputs, 512 to 16384 of K; 7 to 14% rms, the few-row kernel
 // up to 17%): the choice made by them is 1.1% slower than the best of all kernels,
 // tiles and splits on average, 16% at the 99th percentile. A workgroup takes max(c1, c2 n)
-// per step of K, n workgroups to a CU, e more for each beyond the first; parts are
-// written and read once. What the choice is for: 8192 x 8192 at 64 rows fp8 takes
+// per step of K (of its groups' longest), n workgroups to a CU, e more for each beyond
+// the first; parts are written and read once. What the choice is for: 8192 x 8192 at 64 rows fp8 takes
 // 15.9 us in the few-row kernel, 16.4 in tiles of 64 x 128 over 4 splits and 22.9
 // without; 28672 outputs there 55, 36 (2 splits) and 30; 8192 outputs of K 3584 at 1000
 // rows 28 in tiles of 64 x 512, 32 of 64 x 128, 41 of 128 x 512; 14336 of K 8192 at 2048
 // rows 204, 230 and 172.
+// A row of 64 x 128 is of the plain product or, with two groups of waves over K, of the
+// gated one, which no 64 x 64 serves.
+enum Uses { kPlain = 1, kGated = 2, kBoth = 3 };
 struct TileCost {
-  int kind, bm, bn;
+  int kind, uses, bm, bn, groups;
   double start, c1, c2, e, reduce, mb;
 };
-constexpr TileCost kTileFp8[] = {
-    {kMxTiles128x512, 128, 512, 8.4, 0.71, 1.12, 1.0, 5.0, 6.7e6}, {kMxTiles64x512, 64, 512, 5.0, 0.00, 0.674, 2.9, 3.4, 5.2e6},
-    {kMxTiles64x256, 64, 256, 4.4, 0.18, 0.354, 1.5, 3.2, 4.8e6},  {kMxTiles128x256, 128, 256, 6.9, 0.43, 0.61, 0.5, 4.8, 7.1e6},
-    {kMxTiles64x128, 64, 128, 3.7, 0.05, 0.230, 0.9, 3.0, 4.4e6}};
-constexpr TileCost kTileFp4[] = {
-    {kMxTiles128x512, 128, 512, 8.3, 0.00, 0.676, 8.6, 6.4, 8.5e6}, {kMxTiles64x512, 64, 512, 4.5, 0.00, 0.546, 2.6, 3.8, 5.4e6},
-    {kMxTiles64x256, 64, 256, 4.2, 0.01, 0.257, 2.0, 3.4, 5.2e6},   {kMxTiles128x256, 128, 256, 6.2, 0.24, 0.400, 1.5, 5.0, 7.0e6},
-    {kMxTiles64x128, 64, 128, 3.5, 0.10, 0.163, 1.0, 3.2, 4.6e6}};
+constexpr TileCost kTileFp8[] = {{kMxTiles128x512, kBoth, 128, 512, 1, 8.4, 0.71, 1.12, 1.0, 5.0, 6.7e6},
+                                 {kMxTiles64x512, kBoth, 64, 512, 1, 5.0, 0.00, 0.674, 2.9, 3.4, 5.2e6},
+                                 {kMxTiles64x256, kBoth, 64, 256, 1, 4.4, 0.18, 0.354, 1.5, 3.2, 4.8e6},
+                                 {kMxTiles128x256, kBoth, 128, 256, 1, 6.9, 0.43, 0.61, 0.5, 4.8, 7.1e6},
+                                 {kMxTiles64x128, kPlain, 64, 128, 1, 3.7, 0.05, 0.230, 0.9, 3.0, 4.4e6},
+                                 {kMxTiles64x128, kGated, 64, 128, 2, 5.5, 0.235, 0.406, 4.3, 3.0, 4.4e6},
+                                 {kMxTiles64x64, kPlain, 64, 64, 2, 4.9, 0.25, 0.314, 3.2, 3.0, 4.4e6}};
+constexpr TileCost kTileFp4[] = {{kMxTiles128x512, kBoth, 128, 512, 1, 8.3, 0.00, 0.676, 8.6, 6.4, 8.5e6},
+                                 {kMxTiles64x512, kBoth, 64, 512, 1, 4.5, 0.00, 0.546, 2.6, 3.8, 5.4e6},
+                                 {kMxTiles64x256, kBoth, 64, 256, 1, 4.2, 0.01, 0.257, 2.0, 3.4, 5.2e6},
+                                 {kMxTiles128x256, kBoth, 128, 256, 1, 6.2, 0.24, 0.400, 1.5, 5.0, 7.0e6},
+                                 {kMxTiles64x128, kPlain, 64, 128, 1, 3.5, 0.10, 0.163, 1.0, 3.2, 4.6e6},
+                                 {kMxTiles64x128, kGated, 64, 128, 2, 4.6, 0.235, 0.307, 1.4, 3.2, 4.6e6},
+                                 {kMxTiles64x64, kPlain, 64, 64, 2, 4.3, 0.12, 0.217, 1.2, 3.2, 4.6e6}};
 // The few-row kernel: start + n (workgroups to a CU) iter (chunks a wave takes) +
 // wave (waves), by rows up to 16, 32, 64
 struct RowsCost {
@@ -265,16 +274,14 @@ MxPlan plan_mx(int M, int N, int K, int fmt, bool gated, bool quant) {
     }
   }
   for (const TileCost& c : fp4 ? kTileFp4 : kTileFp8) {
-    // the gated product has a tile of each projection per wave; 128 rows with half
-    // of them empty never pay
-    if (gated && c.kind == kMxTiles64x128) continue;
-    if (c.bm > 64 && M <= 64) continue;
+    if (!(c.uses & (gated ? kGated : kPlain))) continue;
+    if (c.bm > 64 && M <= 64) continue;  // half of the rows empty never pay
     const int64_t wgs = (int64_t)up(M, c.bm) * up((int64_t)N * weights, c.bn);
     const int block = !fp4 && c.bm == 128 ? 2 : 4, blocks = up(steps, block);
     for (int ks : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
       if (ks > blocks || (ks > 1 && (wgs * ks > 3 * kCus || (int64_t)ks * M * N * 4 * weights > kMxPartBytes))) break;
       const int n = up(wgs * ks, kCus);
-      double t = c.start + (double)(up(blocks, ks) * block) * std::max(c.c1, c.c2 * n) + c.e * (n - 1);
+      double t = c.start + (double)(up(blocks, ks * c.groups) * block) * std::max(c.c1, c.c2 * n) + c.e * (n - 1);
       if (ks > 1) t += c.reduce + (double)ks * M * N * weights * 8 / c.mb;
       // (3,000 gated launches: the choice 1.1% from the best so, 1.4 without; the first
       // product of 8192 / 3584 / 8192 at 1000 rows 53.5 us here, 49.3 in tiles of 64 x 512)

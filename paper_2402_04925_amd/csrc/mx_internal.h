@@ -91,7 +91,7 @@ struct MxArgs {
 // How a product runs: the few-row kernel over whole or half tiles of 32 outputs, or
 // tiles of rows x weight rows (gated: half of them of each projection) with K split
 // over ks workgroups (fp32 parts, added in the splits' order by a second kernel).
-enum MxKind { kMxRows, kMxRowsHalf, kMxTiles128x512, kMxTiles64x512, kMxTiles64x256, kMxTiles128x256, kMxTiles64x128 };
+enum MxKind { kMxRows, kMxRowsHalf, kMxTiles128x512, kMxTiles64x512, kMxTiles64x256, kMxTiles128x256, kMxTiles64x128, kMxTiles64x64 };
 struct MxPlan {
   int kind, ks;
 };

@@ -1,9 +1,14 @@
 // Product of microscaled (MX) operands with many rows of X on gfx950: the matrix
 // pipe bounds it (mx_gemm.hip has the few-row kernel and the operands' layout).
 //
-// A workgroup of NW waves computes 16 RT rows x 32 NP NW outputs (GATED: NP = 2, a
+// A workgroup of NW KG waves computes 16 RT rows x 32 NP NW outputs (GATED: NP = 2, a
 // tile of the gate and one of the up projection per wave), a wave all of the rows,
-// RT x 2 NP accumulators. K advances a block of S instruction steps of 128 at a time:
+// RT x 2 NP accumulators. Small tiles are worked by KG groups of NW waves, each over a
+// part of K with LDS of its own and added there at the end, which gives a CU twice the
+// loads in flight and needs no second kernel for the sum (gated, 1792 outputs of K 4096 at
+// 400 rows fp8 13.5 us, in tiles of 64 x 256 17.2; 3584 of K 8192 at 100 rows fp4 15.3,
+// in those over 4 splits 17.4). K advances a block of S instruction steps of 128 at a
+// time:
 //   * X's codes and scales of block b + 1 go from global memory straight to the
 //     other of two LDS stages while block b is multiplied; one barrier per block. A
 //     load takes 8 rows of a 128-byte line; loads laid out as the operand itself, 16
@@ -28,8 +33,8 @@
 namespace tpdq {
 namespace {
 
-template <int DT, int FMT, int RT, int NP, int NW, int S, bool GATED, bool QUANT>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_mx_tiles(MxArgs a) {
+template <int DT, int FMT, int RT, int NP, int NW, int KG, int S, bool GATED, bool QUANT>
+__global__ __launch_bounds__(NW * KG * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_mx_tiles(MxArgs a) {
   static_assert(!GATED || NP == 2, "a tile of the gate and one of the up projection");
   constexpr int NT = 2 * NP;  // operands per wave
   constexpr int XW = FMT == kFp4 ? 1 : 2;      // 64-byte halves of a row's line per step
@@ -42,9 +47,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr int XBYTES = BM * REC * 64;
   constexpr int STAGE = XBYTES + SREC * 256;
   constexpr int ITEMS = XREC + SPW;              // loads to LDS per wave and block
+  static_assert(RT % KG == 0, "a wave finishes whole row tiles");
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = KG > 1 ? wave_all / NW : 0;  // the wave's group, with LDS stages of its own
+  const int wave = wave_all - kg * NW;
+  unsigned char* const stages = smem + kg * 2 * STAGE;
   const int r16 = lane & 15, g = lane >> 4;
   const int nbm = (a.M + BM - 1) / BM;
   const int ks = a.ks;
@@ -63,8 +72,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int chunks = (a.K + kMxChunk - 1) / kMxChunk;
   const int tiles = (a.N + kMxTile - 1) / kMxTile;
   const int nblk_all = (steps + S - 1) / S;
-  const int kb0 = (int)((int64_t)nblk_all * kidx / ks);  // this workgroup's blocks
-  const int nblk = (int)((int64_t)nblk_all * (kidx + 1) / ks);
+  const int wg0 = (int)((int64_t)nblk_all * kidx / ks);  // this workgroup's blocks
+  const int wg1 = (int)((int64_t)nblk_all * (kidx + 1) / ks);
+  // and the group's; all groups go through as many, the last one's past its end being zeros
+  const int per_group = (wg1 - wg0 + KG - 1) / KG;
+  const int kb0 = wg0 + kg * per_group, kb1 = kb0 + per_group;
+  const int nblk = min(wg1, kb1);
 
   // Rows past M and tiles past the last one load zeros from the resource bounds
   // (an offset that stays out of range whatever block is added to it); steps past
@@ -99,7 +112,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   // All loads are unconditional and their conditions selects: a branch inside the
   // block would let the compiler move the matrix instructions past it.
   auto dma_item = [&](int b, int st, int k) {
-    unsigned char* sb = smem + st * STAGE;
+    unsigned char* sb = stages + st * STAGE;
     if (k < XREC) {
       const int line = (XREC * wave + k) % REC / 2;
       const bool in = (b < nblk) & (S * b + 2 * line / XW < steps);
@@ -152,13 +165,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 
   int st = 0;
 #pragma unroll 1
-  for (int b = kb0; b < nblk; ++b) {
+  for (int b = kb0; b < kb1; ++b) {
     // this wave's LDS loads of block b (and its scale words) have landed, the
     // weight loads issued after them may be in flight; the barrier publishes
     // every wave's and frees the other stage
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(NT * S) : "memory");
-    const unsigned char* xb = smem + st * STAGE;
-    const unsigned char* sb = smem + st * STAGE + XBYTES + r16 * 4 + g + (S == 2 ? 128 * (b & 1) : 0);
+    const unsigned char* xb = stages + st * STAGE;
+    const unsigned char* sb = stages + st * STAGE + XBYTES + r16 * 4 + g + (S == 2 ? 128 * (b & 1) : 0);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       ws[p] = wsn[p];
@@ -213,17 +226,40 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   // the loads past the last block (zeros) still write LDS: let them land
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
+  // Groups: the sums of row tile r go through LDS, added in the groups' order by group r % KG
+  f4_t* red = (f4_t*)smem;  // [group][wave][RT * NT][64]
+  if constexpr (KG > 1) {
+    __syncthreads();
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) red[((kg * NW + wave) * RT * NT + r * NT + i) * 64 + lane] = acc[r][i];
+    __syncthreads();
+  }
+#pragma unroll
+  for (int q = 0; q < RT / KG; ++q) {
+    const int r = q * KG + kg;
     const int m = row0 + r * 16 + r16;
+    f4_t y[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      if constexpr (KG == 1) {
+        y[i] = acc[q][i];
+      } else {
+        const f4_t* p = red + (wave * RT * NT + r * NT + i) * 64 + lane;
+        y[i] = p[0];
+#pragma unroll
+        for (int k = 1; k < KG; ++k) y[i] += p[k * NW * RT * NT * 64];
+      }
+    }
     if (ks > 1) {  // this split's part, [split][(gate, up)][M][N]
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
         const int64_t n = (int64_t)(GATED ? T0 : T0 + p) * kMxTile + 8 * g;
         float* part = a.part + ((int64_t)(GATED ? 2 * kidx + p : kidx) * a.M + m) * a.N + n;
         if (m < a.M && n < a.N) {
-          *(f4_t*)part = acc[r][2 * p];
-          *(f4_t*)(part + 4) = acc[r][2 * p + 1];
+          *(f4_t*)part = y[2 * p];
+          *(f4_t*)(part + 4) = y[2 * p + 1];
         }
       }
       continue;
@@ -233,8 +269,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float y = acc[r][2 * p + (e >> 2)][e & 3];
-        v[e] = GATED ? silu_mul(y, acc[r][2 + (e >> 2)][e & 3]) : y;
+        const float o = y[2 * p + (e >> 2)][e & 3];
+        v[e] = GATED ? silu_mul(o, y[2 + (e >> 2)][e & 3]) : o;
       }
       store_out8<DT, FMT, QUANT>(a, v, m, (int64_t)(T0 + p) * kMxTile + 8 * g);
     }
@@ -277,18 +313,20 @@ __global__ __launch_bounds__(256) void k_mx_reduce(MxArgs a, int64_t octets, int
     *(u4_t*)(a.Y + m * a.ldy + 8 * k8) = pack8<DT>(v[0]);
 }
 
-template <int DT, int FMT, int RT, int NP, int NW, int S, bool GATED, bool QUANT>
+template <int DT, int FMT, int RT, int NP, int NW, int KG, int S, bool GATED, bool QUANT>
 hipError_t tiles_launch(const MxArgs& a, hipStream_t s) {
   constexpr int BM = 16 * RT;
-  constexpr int lds = 2 * BM * (S * (FMT == kFp4 ? 64 : 128) + 16);
-  auto* k = k_mx_tiles<DT, FMT, RT, NP, NW, S, GATED, QUANT>;
+  constexpr int stages = KG * 2 * BM * (S * (FMT == kFp4 ? 64 : 128) + 16), red = KG > 1 ? KG * NW * RT * 2 * NP * 1024 : 0;
+  constexpr int lds = stages > red ? stages : red;
+  static_assert((size_t)lds <= kLdsMax, "");
+  auto* k = k_mx_tiles<DT, FMT, RT, NP, NW, KG, S, GATED, QUANT>;
   static std::atomic<uint64_t> done{0};
   hipError_t e = allow_lds((const void*)k, lds, &done);
   if (e != hipSuccess) return e;
   const int tiles = (int)(QUANT && a.ks == 1 ? mx_chunks(a.N) * (kMxChunk / kMxTile) : (a.N + kMxTile - 1) / kMxTile);
   const int per = (GATED ? 1 : NP) * NW;
   const int64_t grid = (int64_t)((a.M + BM - 1) / BM) * ((tiles + per - 1) / per) * a.ks;
-  k<<<dim3((unsigned)grid), dim3(NW * 64), lds, s>>>(a);
+  k<<<dim3((unsigned)grid), dim3(NW * KG * 64), lds, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.ks == 1) return e;
   const int per_row = QUANT ? (int)(mx_chunks(a.N) * 64) : a.N / 8;
@@ -301,13 +339,15 @@ template <int DT, int FMT, bool GATED, bool QUANT>
 hipError_t tiles_pick(const MxArgs& a, int kind, hipStream_t s) {
   constexpr int S2 = FMT == kFp4 ? 4 : 2;  // fp8, 128 rows: registers for two steps
   switch (kind) {
-    case kMxTiles128x512: return tiles_launch<DT, FMT, 8, 2, 8, S2, GATED, QUANT>(a, s);
-    case kMxTiles64x512: return tiles_launch<DT, FMT, 4, 2, 8, 4, GATED, QUANT>(a, s);
-    case kMxTiles64x256: return tiles_launch<DT, FMT, 4, 2, 4, 4, GATED, QUANT>(a, s);
-    case kMxTiles128x256: return tiles_launch<DT, FMT, 8, 2, 4, S2, GATED, QUANT>(a, s);
+    case kMxTiles128x512: return tiles_launch<DT, FMT, 8, 2, 8, 1, S2, GATED, QUANT>(a, s);
+    case kMxTiles64x512: return tiles_launch<DT, FMT, 4, 2, 8, 1, 4, GATED, QUANT>(a, s);
+    case kMxTiles64x256: return tiles_launch<DT, FMT, 4, 2, 4, 1, 4, GATED, QUANT>(a, s);
+    case kMxTiles128x256: return tiles_launch<DT, FMT, 8, 2, 4, 1, S2, GATED, QUANT>(a, s);
+    // two groups of waves; of the gated product 64 outputs as well
+    case GATED ? kMxTiles64x128 : kMxTiles64x64: return tiles_launch<DT, FMT, 4, GATED ? 2 : 1, 2, 2, 4, GATED, QUANT>(a, s);
   }
   if constexpr (!GATED)
-    if (kind == kMxTiles64x128) return tiles_launch<DT, FMT, 4, 1, 4, 4, GATED, QUANT>(a, s);
+    if (kind == kMxTiles64x128) return tiles_launch<DT, FMT, 4, 1, 4, 1, 4, GATED, QUANT>(a, s);
   return hipErrorInvalidValue;
 }
 

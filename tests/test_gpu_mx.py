@@ -350,7 +350,8 @@ def test_product_of_real_layers(fmt, M, N, K):
 # ragged sizes (K and N in no whole block, step, chunk or tile) that reach every tile
 # shape, in 16 bits, quantized and gated (tests/test_mx_ref.py checks that they do)
 TILES = [(1155, 8984, 328), (1421, 2976, 456), (223, 8248, 584), (1639, 4632, 1160), (2040, 8184, 1032), (1526, 5400, 904),
-         (43, 40, 2680), (40, 14344, 1160), (30, 4360, 1096), (100, 360, 5000)]
+         (43, 40, 2680), (40, 14344, 1160), (30, 4360, 1096), (100, 360, 5000),
+         (101, 968, 2632), (149, 240, 3088), (1027, 136, 10072), (100, 1016, 1176), (593, 6480, 192)]
 
 
 def some_rows(M, seed):

@@ -61,18 +61,19 @@ def test_the_gpu_tests_reach_every_kernel(lib):
     from tests import test_gpu_mx as t
     plan = getattr(lib, "_ZN4tpdq7plan_mxEiiiibb")  # MxPlan plan_mx(M, N, K, fmt, gated, quant)
     plan.restype, plan.argtypes = ctypes.c_int64, [ctypes.c_int] * 4 + [ctypes.c_bool] * 2
-    rows, half, t128x512, t64x512, t64x256, t128x256, t64x128 = range(7)
+    rows, half, t128x512, t64x512, t64x256, t128x256, t64x128, t64x64 = range(8)
     for fmt in (ref.FP4, ref.FP8):
         seen = {}
         for gated, quant in ((False, False), (False, True), (True, True)):
             for M, N, K in t.TILES + ([] if quant else t.SHAPES + t.LARGE):
                 p = plan(M, N, K, fmt, gated, quant)
                 seen.setdefault((gated, quant), set()).add((p & 0xFFFFFFFF, (p >> 32) > 1))
-        tiles = {t128x512, t64x512, t64x256, t128x256, t64x128}
+        tiles = {t128x512, t64x512, t64x256, t128x256, t64x128, t64x64}
         assert {k for k, _ in seen[False, False]} == tiles | {rows, half}
         assert {k for k, _ in seen[False, True]} == tiles | {rows}
-        assert {k for k, _ in seen[True, True]} == tiles - {t64x128} | {rows}
+        assert {k for k, _ in seen[True, True]} == tiles - {t64x64} | {rows}
         assert all(any(split for _, split in kinds) for kinds in seen.values())
+        assert {(t64x128, False), (t64x128, True)} <= seen[True, True]  # two groups of waves
 
 
 # ---- refusals ------------------------------------------------------------
