@@ -217,7 +217,8 @@ class QuantWeight:
 
 class Workspace:
     """Device scratch for the library calls, grown on demand. One workspace
-    serves any number of calls issued one after another on one stream."""
+    serves any number of calls issued one after another on one stream. Made
+    without a device, it takes that of the first call that it is given to."""
 
     def __init__(self, device=None):
         self.device = device
@@ -240,7 +241,12 @@ def _workspace(device, nbytes, ws: Optional[Workspace]):
         ws = _default_ws.get(key)
         if ws is None:
             ws = _default_ws[key] = Workspace(device)
-    return ws.get(nbytes)
+    elif ws.device is None and ws.buf is None:
+        ws.device = device
+    buf = ws.get(nbytes)
+    if buf.device != device:  # kernels write it
+        raise ValueError(f"the workspace is on {buf.device}, the call's tensors on {device}")
+    return buf
 
 
 def workspace_bytes(op: int, M: int, a: QuantWeight, b: Optional[QuantWeight] = None) -> int:

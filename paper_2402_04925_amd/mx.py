@@ -12,7 +12,7 @@ import functools
 from typing import Optional
 
 from . import _abi
-from . import Workspace, _dtype_code, _stream_handle, _torch
+from . import Workspace, _dtype_code, _stream_handle, _torch, _workspace
 from ._abi import MX_FP4, MX_FP8, MX_ROWS, MX_TILED
 
 _BLOCK, _STEP, _CHUNK, _TILE = 32, 128, 512, 32
@@ -289,7 +289,10 @@ def _scratch(workspace: Optional[Workspace], nbytes: int, device):
     streams, share none."""
     if not nbytes:
         return None, 0, None
-    buf = workspace.get(nbytes) if workspace is not None else _torch().empty(nbytes, dtype=_torch().uint8, device=device)
+    if workspace is None:
+        buf = _torch().empty(nbytes, dtype=_torch().uint8, device=device)
+    else:
+        buf = _workspace(device, nbytes, workspace)
     return buf.data_ptr(), buf.numel(), buf
 
 
