@@ -127,10 +127,19 @@ class MxTensor:
 
     @classmethod
     def from_tensors(cls, codes, scales, K: int, fmt: int) -> "MxTensor":
-        """An MX_ROWS tensor from dense codes ([R][ceil(K/32) * 32] fp8, half as
-        many bytes for fp4) and scales ([R][ceil(K/32)], uint8 or float8_e8m0fnu),
-        copied into padded rows. Codes at and past K count as zeros."""
+        """An MX_ROWS tensor from dense codes ([R][ceil(K/32) * 32] fp8, float8_e4m3fn
+        or its bytes as uint8; half as many bytes for fp4, uint8 or float4_e2m1fn_x2)
+        and scales ([R][ceil(K/32)], uint8 or float8_e8m0fnu), copied into padded rows.
+        Codes at and past K count as zeros."""
         torch = _torch()
+        own = {MX_FP8: torch.float8_e4m3fn, MX_FP4: getattr(torch, "float4_e2m1fn_x2", torch.uint8)}
+        if fmt not in own:
+            raise ValueError(f"unknown format {fmt}")
+        if codes.dtype not in (torch.uint8, own[fmt]) or scales.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+            raise TypeError(f"codes must be uint8 or {own[fmt]} and scales uint8 or float8_e8m0fnu, got {codes.dtype} and "
+                            f"{scales.dtype}")
+        if scales.device != codes.device:
+            raise ValueError(f"scales are on {scales.device}, codes on {codes.device}")
         blocks, R = _up(K, _BLOCK), codes.shape[0]
         per = 16 if fmt == MX_FP4 else 32
         if K < 1 or K % 8 or tuple(codes.shape) != (R, blocks * per) or tuple(scales.shape) != (R, blocks):

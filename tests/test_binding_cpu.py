@@ -37,3 +37,44 @@ def test_workspace_without_a_device_takes_the_call_s(take, monkeypatch):
     with pytest.raises(ValueError, match="workspace"):  # the stand-in's memory is no GPU's
         take(ws)
     assert made == [GPU] and ws.device == GPU
+
+
+# ---- MxTensor.from_tensors -----------------------------------------------
+
+U8, E8M0 = torch.uint8, torch.float8_e8m0fnu
+CODES = {tpdq.MX_FP8: ([torch.float8_e4m3fn, U8], 64), tpdq.MX_FP4: ([U8, torch.float4_e2m1fn_x2], 32)}
+
+
+def ones(dtype, *shape):
+    """Bytes 1 of a one-byte type, ones of any other."""
+    if dtype.itemsize == 1:
+        return torch.ones(*shape, dtype=U8).view(dtype)
+    return torch.ones(*shape, dtype=dtype)
+
+
+@pytest.mark.parametrize("fmt", [tpdq.MX_FP4, tpdq.MX_FP8])
+def test_from_tensors_takes_the_format_s_types(fmt):
+    types, n = CODES[fmt]
+    for t in types:
+        for s in (U8, E8M0):
+            q = tpdq.MxTensor.from_tensors(ones(t, 2, n), ones(s, 2, 2), 64, fmt)
+            assert (q.codes.view(U8)[:, :n] == 1).all() and (q.scales.view(U8) == 1).all()
+
+
+@pytest.mark.parametrize("fmt", [tpdq.MX_FP4, tpdq.MX_FP8])
+def test_from_tensors_refuses_other_types(fmt):
+    """Their bytes are no codes of the format: a float's, an int32's, another fp8's."""
+    types, n = CODES[fmt]
+    others = [torch.float8_e4m3fnuz, torch.float8_e5m2, torch.int8, torch.bool, torch.float16, torch.int32, torch.float32,
+              torch.int64] + ([torch.float8_e4m3fn] if fmt == tpdq.MX_FP4 else [torch.float4_e2m1fn_x2])
+    for t in others:
+        with pytest.raises(TypeError):
+            tpdq.MxTensor.from_tensors(ones(t, 2, n), ones(U8, 2, 2), 64, fmt)
+    for t in (torch.int8, torch.bool, torch.float8_e4m3fn, torch.float16, torch.float32, torch.int32):
+        with pytest.raises(TypeError):
+            tpdq.MxTensor.from_tensors(ones(types[0], 2, n), ones(t, 2, 2), 64, fmt)
+
+
+def test_from_tensors_refuses_two_devices():
+    with pytest.raises(ValueError, match="device|on "):
+        tpdq.MxTensor.from_tensors(ones(U8, 2, 64), torch.empty(2, 2, dtype=U8, device="meta"), 64, tpdq.MX_FP8)
