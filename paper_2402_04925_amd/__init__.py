@@ -79,6 +79,8 @@ def _check_args(device, scales_dtype=None, **tensors):
         if name in ("x_perm", "P1") and (t.dtype != torch.int32 or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous int32 tensor")
     X = tensors.get("X")
+    if X is not None and X.shape[0] > _abi.COUNT_MAX:
+        _abi.check_counts(M=X.shape[0])
     if X is not None and scales_dtype is not None and X.dtype != scales_dtype:
         raise TypeError(f"X is {X.dtype} but the scales are {scales_dtype}: one element type per call")
 
@@ -140,10 +142,11 @@ class QuantWeight:
         q, s, z, g = self.qweight, self.scales, self.qzeros, self.g_idx
         # every condition of the loops below in one expression (a call makes one
         # to three of these); they say which one does not hold
-        i32, dev = torch.int32, q.device
+        i32, dev, most = torch.int32, q.device, _abi.COUNT_MAX
         if not (q.dtype is i32 and z.dtype is i32 and (s.dtype is torch.float16 or s.dtype is torch.bfloat16)
                 and s.device == dev and z.device == dev
                 and q.stride(1) == 1 and s.stride(1) == 1 and z.stride(1) == 1
+                and self.K <= most and self.N <= most and self.G <= most and self.num_groups <= most
                 and (g is None or (g.dtype is i32 and g.device == dev and g.is_contiguous()))):
             self._check_tensors()
         if path == PATH_ORDERED and self.G > 0:
@@ -155,6 +158,7 @@ class QuantWeight:
 
     def _check_tensors(self):
         torch = _torch()
+        _abi.check_counts(K=self.K, N=self.N, G=self.G, num_groups=self.num_groups)
         for name in ("qweight", "scales", "qzeros", "g_idx"):
             t = getattr(self, name)
             if t is None:
@@ -250,6 +254,7 @@ def _workspace(device, nbytes, ws: Optional[Workspace]):
 
 
 def workspace_bytes(op: int, M: int, a: QuantWeight, b: Optional[QuantWeight] = None) -> int:
+    _abi.check_counts(M=M)
     ca = a.c_struct()
     cb = b.c_struct() if b is not None else None
     return _abi.lib().tpdq_workspace_bytes(op, M, ctypes.byref(ca),

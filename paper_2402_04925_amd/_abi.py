@@ -16,6 +16,17 @@ MX_FP4, MX_FP8 = 0, 1
 MX_ROWS, MX_TILED = 0, 1
 OP_MX_GEMM, OP_MX_MLP = 0, 1  # of tpdq_mx_workspace_bytes
 
+# Sizes are int32 in the C ABI, and ctypes keeps the low 32 bits of a larger one
+# without an error: the binding refuses those itself.
+COUNT_MAX = (1 << 31) - 1
+
+
+def check_counts(**counts):
+    for name, n in counts.items():
+        if n > COUNT_MAX:
+            raise ValueError(f"{name}={n}: sizes are below 2^31")
+
+
 EXPORTED = (
     "tpdq_reorder", "tpdq_pack_tiled", "tpdq_w4a16_gemm", "tpdq_mlp_shard", "tpdq_mlp_shard_noalloc",
     "tpdq_gated_mlp_shard",

@@ -55,6 +55,8 @@ def _rows16(name, t, M=None, K=None, dtype=None):
     """A 16-bit matrix with unit column stride (M x K, of dtype)."""
     if t.dim() != 2 or t.stride(1) != 1:
         raise ValueError(f"{name} must be 2-D with unit column stride")
+    if M is None and (t.shape[0] > _abi.COUNT_MAX or t.shape[1] > _abi.COUNT_MAX):
+        _abi.check_counts(rows=t.shape[0], columns=t.shape[1])
     if M is not None and (t.shape[0] != M or t.shape[1] != K):
         raise ValueError(f"{name} must be [{M}][{K}], got {list(t.shape)}")
     if dtype is not None and t.dtype != dtype:
@@ -75,6 +77,7 @@ class MxTensor:
 
     def __init__(self, codes, padded_scales, R: int, K: int, fmt: int, layout: int = MX_ROWS):
         torch = _torch()
+        _abi.check_counts(R=R, K=K)
         c, s = codes, padded_scales
         rows = R if layout == MX_ROWS else _up(R, _TILE)
         dev = c.device
@@ -115,6 +118,8 @@ class MxTensor:
         """Storage for mx_quantize, rmsnorm or mx_pack to write. (Sizes go to torch apart: as
         a tuple an allocation takes 1.6 us, so 1.3.)"""
         torch = _torch()
+        if R > _abi.COUNT_MAX or K > _abi.COUNT_MAX:
+            _abi.check_counts(R=R, K=K)
         per_c, per_s = cls._widths(fmt, layout)
         c, s = -(-K // _STEP) * per_c, -(-K // _CHUNK) * per_s
         t = torch.float8_e4m3fn if fmt == MX_FP8 else torch.uint8

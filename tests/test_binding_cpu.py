@@ -1,4 +1,6 @@
 """What the binding refuses on the host, before the library is called (no GPU)."""
+import types
+
 import pytest
 import torch
 
@@ -78,3 +80,52 @@ def test_from_tensors_refuses_other_types(fmt):
 def test_from_tensors_refuses_two_devices():
     with pytest.raises(ValueError, match="device|on "):
         tpdq.MxTensor.from_tensors(ones(U8, 2, 64), torch.empty(2, 2, dtype=U8, device="meta"), 64, tpdq.MX_FP8)
+
+
+# ---- counts past the C ABI's 32 bits -------------------------------------
+
+MANY = (1 << 32) + 8  # 8 in its low 32 bits
+
+
+def meta(*shape, dtype=torch.float16):
+    return torch.empty(*shape, dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("layout", [tpdq.MX_ROWS, tpdq.MX_TILED])
+@pytest.mark.parametrize("R,K", [(MANY, 8), (8, MANY), (1 << 31, 8), (8, 1 << 31)])
+def test_mx_sizes_past_32_bits_are_refused(R, K, layout):
+    with pytest.raises(ValueError, match="2\\^31"):
+        tpdq.MxTensor.empty(R, K, tpdq.MX_FP4, "meta", layout)
+    rows = R if layout == tpdq.MX_ROWS else -(-R // 32)
+    per_c, per_s = tpdq.MxTensor._widths(tpdq.MX_FP4, layout)
+    with pytest.raises(ValueError, match="2\\^31"):
+        tpdq.MxTensor(meta(rows, -(-K // 128) * per_c, dtype=U8), meta(rows, -(-K // 512) * per_s, dtype=E8M0), R, K,
+                      tpdq.MX_FP4, layout)
+
+
+def test_largest_mx_size_is_kept():
+    q = tpdq.MxTensor.empty((1 << 31) - 1, 8, tpdq.MX_FP4, "meta")
+    assert (q._c.R, q._c.K) == ((1 << 31) - 1, 8)
+
+
+@pytest.mark.parametrize("shape", [(MANY, 8), (8, MANY)])
+def test_16_bit_rows_past_32_bits_are_refused(shape):
+    x = meta(*shape)
+    with pytest.raises(ValueError, match="2\\^31"):
+        tpdq.rmsnorm(x, meta(shape[1]), 1e-5)
+    with pytest.raises(ValueError, match="2\\^31"):
+        tpdq.mx_quantize(x, tpdq.MX_FP8)
+
+
+def test_w4a16_counts_past_32_bits_are_refused():
+    x = types.SimpleNamespace(device=GPU, shape=(MANY, 8), dtype=torch.float16)
+    with pytest.raises(ValueError, match="2\\^31"):
+        tpdq._check_args(GPU, torch.float16, X=x)
+    for K, N in ((MANY, 8), (8, MANY)):
+        w = tpdq.QuantWeight.from_tensors(meta(K // 8, N, dtype=torch.int32), meta(1, N), meta(1, N // 8, dtype=torch.int32),
+                                          None, K, 1)
+        with pytest.raises(ValueError, match="2\\^31"):
+            w.c_struct()
+    w = tpdq.QuantWeight.from_tensors(meta(1, 8, dtype=torch.int32), meta(1, 8), meta(1, 1, dtype=torch.int32), None, 8, 1)
+    with pytest.raises(ValueError, match="2\\^31"):
+        tpdq.workspace_bytes(tpdq.OP_GEMM, MANY, w)
