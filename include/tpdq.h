@@ -376,10 +376,12 @@ tpdq_status tpdq_mx_pack(const tpdq_mx* src, const tpdq_mx* dst, void* stream);
  * y goes to Y [M][ldy] rounded to dtype (then q is NULL), as tpdq_w4a16_gemm and
  * the MLP shards take it, or to q (TPDQ_MX_ROWS, R = M; then Y is NULL), quantized
  * from fp32 as by tpdq_mx_quantize. X, residual [M][ld] and weight [K] are of
- * dtype. residual_out and Y may each be X or residual itself (every element is read
- * before it is written), but not one another. K a multiple of 8, at most 65536. The
- * sum of squares is taken in fp32: rows of magnitudes past 2^63 / sqrt(K) overflow it,
- * and what lies below 2^-63 adds nothing exact to it (an eps above 2^-100 hides that).
+ * dtype. residual_out and Y may each be X or residual itself, row for row (every
+ * element is read before it is written), but share no other memory with them and none
+ * with one another, nor residual_out with q: TPDQ_ERR_SHAPE. K a multiple of 8, at most
+ * 65536. The sum of squares is taken in fp32: rows of magnitudes past 2^63 / sqrt(K)
+ * overflow it, and what lies below 2^-63 adds nothing exact to it (an eps above 2^-100
+ * hides that).
  * Alignment: every pointer 16 B, every leading dimension % 8 == 0.
  */
 tpdq_status tpdq_rmsnorm(const void* X, int64_t ldx, const void* residual, int64_t ldr, const void* weight,

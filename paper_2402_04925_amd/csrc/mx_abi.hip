@@ -54,6 +54,25 @@ tpdq_status check_rows16(const void* p, int64_t ld, int64_t K, const char* name)
   return TPDQ_OK;
 }
 
+// `rows` rows of `bytes` bytes, `ld` bytes apart
+struct Strip {
+  const void* p;
+  int64_t ld, bytes;
+};
+
+bool same(const Strip& a, const Strip& b, int64_t rows) { return a.p == b.p && (a.ld == b.ld || rows == 1); }
+
+// Whether two strips share memory. With one leading dimension that is exact (columns of
+// one buffer, side by side, do not meet); with two it is whether their extents meet.
+bool meet(const Strip& a, const Strip& b, int64_t rows) {
+  typedef __int128 wide;
+  const wide pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+  if (pa + (wide)(rows - 1) * a.ld + a.bytes <= pb || pb + (wide)(rows - 1) * b.ld + b.bytes <= pa) return false;
+  if (rows == 1 || a.ld != b.ld) return true;
+  const wide d = ((pb - pa) % a.ld + a.ld) % a.ld;  // of b's rows behind a's
+  return d < a.bytes || a.ld - d < b.bytes;
+}
+
 MxRows rows_of(const tpdq_mx* q) { return MxRows{(uint8_t*)q->codes, q->ld_c, (uint8_t*)q->scales, q->ld_s}; }
 
 // A launch has fewer than 2^32 threads. Large calls take one for 32 elements: 16 for
@@ -175,7 +194,6 @@ tpdq_status tpdq_rmsnorm(const void* X, int64_t ldx, const void* residual, int64
     if (st != TPDQ_OK) return st;
   }
   if ((Y == nullptr) == (q == nullptr)) return fail(TPDQ_ERR_NULL, "one of Y and q is given");
-  if (Y && Y == residual_out) return fail(TPDQ_ERR_SHAPE, "Y and residual_out are the same memory");
   if (Y) {
     st = check_rows16(Y, ldy, K, "Y");
   } else {
@@ -187,6 +205,19 @@ tpdq_status tpdq_rmsnorm(const void* X, int64_t ldx, const void* residual, int64
   int vpt = 0;
   if ((int64_t)M * norm_threads(K, q ? q->format : -1, &vpt) >= (int64_t)1 << 32)
     return fail(TPDQ_ERR_UNSUPPORTED, "%d rows: more threads than a launch has, split the rows", M);
+  const Strip x{X, 2 * ldx, 2 * (int64_t)K}, res{residual, 2 * ldr, x.bytes}, h{residual_out, 2 * ldh, x.bytes},
+      y{Y, 2 * ldy, x.bytes};
+  if (residual) {
+    const bool shared = Y ? meet(h, y, M)
+                          : meet(h, Strip{q->codes, q->ld_c, mx_row_codes(K, q->format)}, M) ||
+                                meet(h, Strip{q->scales, q->ld_s, mx_row_scales(K)}, M);
+    if (shared) return fail(TPDQ_ERR_SHAPE, "the output and residual_out share memory");
+  }
+  // in place: the workgroup of a row reads it before it writes that row, and no other
+  for (const Strip& out : {h, y})
+    for (const Strip& in : {x, res})
+      if (out.p && in.p && !same(out, in, M) && meet(out, in, M))
+        return fail(TPDQ_ERR_SHAPE, "Y or residual_out shares memory with rows of X or residual other than its own");
   NormArgs a{};
   a.X = (const uint16_t*)X;
   a.ldx = ldx;

@@ -250,7 +250,8 @@ def mx_pack(q: MxTensor) -> MxTensor:
 def rmsnorm(X, weight, eps: float, residual=None, fmt: Optional[int] = None, residual_out=None, out=None):
     """h = X + residual (rounded to X's type; X itself without one), y = h /
     sqrt(mean(h^2) + eps) * weight. Returns (y, h): y in X's type, or with fmt
-    as an MxTensor; h in residual_out (which may be residual itself) or new."""
+    as an MxTensor; h in residual_out or new. residual_out and out may each be X or
+    residual itself; memory shared otherwise is refused."""
     torch = _torch()
     _rows16("X", X)
     dev, dt = _device_of("X", X), X.dtype
