@@ -222,16 +222,22 @@ class QuantWeight:
 class Workspace:
     """Device scratch for the library calls, grown on demand. One workspace
     serves any number of calls issued one after another on one stream. Made
-    without a device, it takes that of the first call that it is given to."""
+    without a device, it takes that of the first call that it is given to.
+    Outgrown buffers are kept, since a captured graph may still write them; each
+    is at least twice the one before, so that together they are smaller than the last."""
 
     def __init__(self, device=None):
         self.device = device
         self.buf = None
+        self._outgrown = []
 
     def get(self, nbytes: int):
         torch = _torch()
         if self.buf is None or self.buf.numel() < nbytes:
             n = max(nbytes, 1 << 20)
+            if self.buf is not None:
+                self._outgrown.append(self.buf)
+                n = max(n, 2 * self.buf.numel())
             self.buf = torch.empty(n, dtype=torch.uint8, device=self.device)
         return self.buf
 

@@ -1,5 +1,7 @@
 """What the binding refuses on the host, before the library is called (no GPU)."""
+import gc
 import types
+import weakref
 
 import pytest
 import torch
@@ -129,3 +131,18 @@ def test_w4a16_counts_past_32_bits_are_refused():
     w = tpdq.QuantWeight.from_tensors(meta(1, 8, dtype=torch.int32), meta(1, 8), meta(1, 1, dtype=torch.int32), None, 8, 1)
     with pytest.raises(ValueError, match="2\\^31"):
         tpdq.workspace_bytes(tpdq.OP_GEMM, MANY, w)
+
+
+def test_outgrown_buffers_are_kept():
+    """A captured graph still writes the buffer that its calls were given."""
+    ws = tpdq.Workspace("cpu")
+    first = weakref.ref(ws.get(100))
+    assert ws.get(8 << 20).numel() >= 8 << 20 and ws.get(100) is ws.buf
+    gc.collect()
+    assert first() is not None
+    # and they stay few: each is at least twice the one before
+    ws, seen = tpdq.Workspace("cpu"), set()
+    for n in range(1 << 20, 16 << 20, 1 << 16):
+        b = ws.get(n)
+        seen.add((b.data_ptr(), b.numel()))
+    assert len(seen) <= 5 and sum(n for _, n in seen) < 2 * b.numel()
