@@ -1,8 +1,8 @@
 // Product of microscaled (MX) operands on gfx950, Y = X W^T: X in fp8 (E4M3) or
 // fp4 (E2M1) rows, W in fp4 tiles (mx_internal.h), both with one E8M0 scale per 32
 // elements of K. The scaled matrix instruction takes the codes and the scales as
-// they are stored, so nothing is dequantized: an output is one fp32 accumulator,
-// rounded once.
+// they are stored, so nothing is dequantized: an output is a sum of fp32 accumulators
+// (of the waves, groups of waves or splits that share K, in their order), rounded once.
 //
 // The weights are the instruction's first operand and X its second, so that a
 // lane's results are consecutive outputs of one row of X. A tile of 32 weight
@@ -215,9 +215,12 @@ hipError_t rows_of(const MxArgs& a, int kind, int dt, hipStream_t s) {
 // per step of K (of its groups' longest), n workgroups to a CU, e more for each beyond
 // the first; parts are written and read once. What the choice is for: 8192 x 8192 at 64 rows fp8 takes
 // 15.9 us in the few-row kernel, 16.4 in tiles of 64 x 128 over 4 splits and 22.9
-// without; 28672 outputs there 55, 36 (2 splits) and 30; 8192 outputs of K 3584 at 1000
-// rows 28 in tiles of 64 x 512, 32 of 64 x 128, 41 of 128 x 512; 14336 of K 8192 at 2048
-// rows 204, 230 and 172.
+// without (the first two are predicted alike, 14.2, and the splits taken); 28672 outputs
+// there 55, 36 (2 splits) and 30; 8192 outputs of K 3584 at 1000 rows 28 in tiles of 64 x
+// 512, 32 of 64 x 128, 41 of 128 x 512; 14336 of K 8192 at 2048 rows 204, 230 and 172.
+// No term stands for memory: up to 128 rows of many outputs, where the weights' stream
+// bounds every kernel, a prediction can lie under it (28672 outputs at 64 rows 18.4 us,
+// the weights at a copy's rate 24) and the other terms choose.
 // A row of 64 x 128 is of the plain product or, with two groups of waves over K, of the
 // gated one, which no 64 x 64 serves.
 enum Uses { kPlain = 1, kGated = 2, kBoth = 3 };

@@ -21,8 +21,10 @@
 //     them and halved the rows took 196 us where 1 x 8 take 170).
 // 8 waves (two per SIMD) with 128 x 512 outputs run 2048 x 14336 x 8192 in 163 to 178
 // us fp8 (2.7 to 2.95 PFLOP/s, a loop of these instructions alone 4.4) and 106 to 114
-// us fp4 (8.1): the matrix pipe is busy 66 and 57% of the clocks at 1.9 GHz, the rest
-// are the block's barrier and the latencies behind it. A barrier in the middle of the
+// us fp4 (8.1): the matrix pipe is busy 66 and 57% of the clocks at 1.9 GHz. Of the rest an
+// eighth of the machine is idle in the second round (448 tiles on 256 CUs), and most is
+// the operands' loads: without X's, the weights' or both (timing only) fp8 took 161, 149
+// and 138 us, without the block's barrier 163, as with it. A barrier in the middle of the
 // block with three stages (171 and 113 us where this took 165 and 106) and operands
 // read two or three row tiles ahead (no change) were not faster. Smaller tiles fill
 // the CUs at fewer rows (plan_mx).

@@ -197,7 +197,7 @@ class MxTensor:
                         self._R, k, self._fmt, self._layout)
 
 
-def _mx_arg(name, q, device=None, layout=None):
+def _mx_arg(name, q, device=None):
     if not isinstance(q, MxTensor):
         raise TypeError(f"{name} must be an MxTensor, got {type(q).__name__}")
     if q._device.type != "cuda":
@@ -320,8 +320,9 @@ def _out16(out, M, N, dtype, device):
 
 
 def mx_gemm(X: MxTensor, w: MxTensor, dtype, out=None, workspace: Optional[Workspace] = None):
-    """Y = X W^T: X [M][K] fp8 or fp4, w [N][K] fp4 from mx_pack, fp32 accumulation,
-    Y [M][N] rounded once to dtype."""
+    """Y = X W^T: X [M][K] fp8 or fp4, w [N][K] fp4 from mx_pack, Y [M][N] rounded once to
+    dtype. fp32 accumulation; of each 8 consecutive products with an fp8 X, what lies 13
+    bits below the largest is dropped (about 1e-4 of a typical output)."""
     cx = _mx_arg("X", X)
     dev = X._device
     cw = _mx_arg("w", w, dev)
@@ -336,7 +337,8 @@ def mx_mlp_shard(X: MxTensor, w_up: MxTensor, w_down: MxTensor, dtype, w_gate: O
                  workspace: Optional[Workspace] = None):
     """One rank's MLP share up to the AllReduce: Y1 = X W_up^T, or silu(X W_gate^T)
     * (X W_up^T) with w_gate, quantized in X's format; returns Y2_partial = Y1
-    W_down^T. w_up and w_gate are column shards, w_down a row shard."""
+    W_down^T. w_up and w_gate are column shards, w_down a row shard. Sums as in
+    mx_gemm; what an fp8 X loses there can change codes of Y1 (see include/tpdq.h)."""
     cx = _mx_arg("X", X)
     dev = X._device
     cu, cd = _mx_arg("w_up", w_up, dev), _mx_arg("w_down", w_down, dev)
